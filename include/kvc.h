@@ -71,6 +71,10 @@ extern "C" {
 #define KVC_SOLVER_DP 1       /* C1 + exact integer DP over per-head budgets */
 #define KVC_SOLVER_C1_ONLY 2  /* C1 at the uniform budget bpd*d (V side; "w/o C2" ablation) */
 
+#define KVC_F16 0
+#define KVC_BF16 1
+#define KVC_F32 2
+
 #define KVC_TILE_TOKENS 64
 #define KVC_HEAD_DIM 128
 
@@ -337,6 +341,89 @@ int kvc_encode_kv(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint
  *  out   device f32 [n_units][n_tok][d]. Async.
  */
 int kvc_reconstruct(const kvc_stream_desc* s, int32_t t0, int32_t n_tok, float* out, void* stream);
+
+/*
+ * Verify step of speculative decoding. A model drafts a tree of up to 64 tokens per sequence, scores all of
+ * them in one pass over the cache and keeps those it accepts. Per layer: kvc_norm_rope lays out the drafted
+ * tokens' projections, kvc_tree_attn attends, and once the tokens are accepted kvc_append_rows stores them.
+ * Keys are cached before their rotation (Sec. 5); the drafted tokens' own keys and values are not
+ * compressed until they are accepted, so nothing has to be taken back for the others.
+ */
+
+/* Drafted tokens per unit at most (one bit each of a row's mask), and query heads per KV head. */
+#define KVC_TREE_MAX_TOKENS 64
+#define KVC_TREE_MAX_GROUP 16
+
+/*
+ * kvc_norm_rope - per-head norm and rotary embedding of a layer's projections, laid out by unit.
+ *  q, k, v     device, token major: token n of sequence s has its heads (kv_heads G for q, kv_heads for k and
+ *              v, d values each) at x + (s n_tok + n) stride elements, so that the three may be parts of one
+ *              projection. 16-byte aligned, strides multiples of 16 bytes. Each may be NULL, with its outputs.
+ *  dtype       KVC_F16, KVC_BF16 or KVC_F32, of q, k and v alike.
+ *  wq, wk      device f32 [d], 16-byte aligned: x is first normalised, y = x / sqrt(mean(x^2) + eps) * w; NULL: y = x.
+ *  pos         device int32 [n_seq][n_tok]: positions (any value; tokens of a tree may share one).
+ *  rope_base   as kvc_decode_attn_rope, or 0: no rotation (pos may then be NULL).
+ *  q_out       device fp16 [n_seq kv_heads][n_tok][G][d]: the rotated queries (query head h G + g of unit
+ *              s kv_heads + h is head g of its unit).
+ *  k_out       device fp16 [n_seq kv_heads][n_tok][d]: the keys before rotation, what the encoder takes.
+ *  k_rot       device fp16, same shape: the rotated keys, what kvc_tree_attn takes. Either may be NULL.
+ *  v_out       device fp16, same shape: the values.
+ * fp32 inside, one rounding to nearest even at the end; values past the fp16 range become +-65504 (the
+ * encoder takes finite input). Outputs are 16-byte aligned and overlap no input. Async on `stream`.
+ */
+int kvc_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  int32_t dtype, int32_t n_seq, int32_t n_tok, int32_t kv_heads, int32_t G, const float* wq,
+                  const float* wk, float eps, const int32_t* pos, float rope_base, uint16_t* q_out, uint16_t* k_out,
+                  uint16_t* k_rot, uint16_t* v_out, void* stream);
+
+/*
+ * kvc_tree_attn - attention of a tree of drafted tokens over the compressed cache and over itself.
+ *  q           device fp16 [n_units][n_tok][G][d], 16-byte aligned: the queries, rotated if the model rotates.
+ *  G           1..KVC_TREE_MAX_GROUP; n_tok: 1..KVC_TREE_MAX_TOKENS.
+ *  xk, xv      device fp16: the drafted tokens' keys (rotated like the queries) and values, token m of unit u
+ *              at x + u unit_stride + m d; 16-byte aligned, strides multiples of 8 elements and >= n_tok d.
+ *  mask        device uint64 [n_units][n_tok]: bit m of word n set: token n attends to drafted token m (its
+ *              ancestors and itself; (2 << n) - 1 is a chain). Bits from n_tok on are ignored. Rows of a
+ *              padded batch may hold 0. A drafted token that no word of its unit names is not read (its key
+ *              and value may hold anything); the others must be finite.
+ *  seq_len     device int32 [n_units]: cached tokens of each unit, all of them visible to every row; clamped
+ *              to [0, max_seq_len] on the device.
+ *  max_seq_len host: 0 <= max_seq_len <= both capacities.
+ *  rope_base   as kvc_decode_attn_rope: the cached key of stream index t is rotated by t after its
+ *              reconstruction; 0: the cached keys are not rotated.
+ *  out         device fp16 [n_units][n_tok][G][d], 16-byte aligned:
+ *              out[u][n][g] = P_V^T sum_t p_t z_V,t + sum_m p_m xv_m,
+ *              p = softmax over the visible t (q . k_t / sqrt(d)) and m (q . xk_m / sqrt(d));
+ *              0 in a row that sees nothing.
+ *  ws          device workspace of >= kvc_tree_attn_workspace(...) bytes, 256-byte aligned, contents ignored.
+ * Softmax statistics and sums are fp32; rotated cached keys and softmax weights are rounded to fp16, like the
+ * result. No atomics: results are deterministic. Async on `stream`.
+ */
+int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* q, int32_t G, int32_t n_tok,
+                  const uint16_t* xk, int64_t xk_unit_stride, const uint16_t* xv, int64_t xv_unit_stride,
+                  const uint64_t* mask, const int32_t* seq_len, int32_t max_seq_len, float rope_base, uint16_t* out,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes kvc_tree_attn needs (host only; 0 on an error). */
+size_t kvc_tree_attn_workspace(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok,
+                               int32_t max_seq_len);
+
+/*
+ * kvc_append_rows - append chosen tokens to every unit's streams, each unit at its own length.
+ *  xk, xv      device fp16 [n_units][...]: row m of unit u at x + u unit_stride + m d, n_rows rows; 16-byte
+ *              aligned, strides multiples of 8 elements and >= n_rows d.
+ *  rows        device int32 [n_units][max_n]: the rows to append, in order; NULL: rows 0, 1, .. (max_n <= n_rows).
+ *  t0          device int32 [n_units]: position of a unit's first new token.
+ *  n           device int32 [n_units]: how many it appends (0: none).
+ *  max_n       host: upper bound of n, 0 <= max_n <= both capacities.
+ * Unit u's row rows[u][i] is encoded at position t0[u] + i, i < n[u], with the codes of kvc_encode. Being device
+ * data, rows, t0 and n are not validated: n is clamped to [0, max_n], a row index to [0, n_rows - 1], and
+ * positions outside [0, capacity) are left out. Streams of different units must not overlap. Every other
+ * token's codes are preserved. Async on `stream`.
+ */
+int kvc_append_rows(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* xk, int64_t xk_unit_stride,
+                    const uint16_t* xv, int64_t xv_unit_stride, int32_t n_rows, const int32_t* rows, const int32_t* t0,
+                    const int32_t* n, int32_t max_n, void* stream);
 
 /*
  * kvc_read_probe - measurement utility, not a step of the method: streams `bytes` bytes of device

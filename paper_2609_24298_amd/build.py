@@ -41,7 +41,7 @@ def build(verbose: bool = True) -> str:
     # the HIP sources compile in parallel (the two decode partials units take most of the time)
     procs = []
     for src in ("kvc_decode_g4.hip", "kvc_decode_g8.hip", "kvc_decode.hip", "kvc_rope_g4.hip", "kvc_rope_g8.hip",
-                "kvc_rope.hip", "kvc_recon.hip", "kvc_kernels.hip", "kvc_calib.hip"):
+                "kvc_rope.hip", "kvc_tree.hip", "kvc_recon.hip", "kvc_kernels.hip", "kvc_norm_rope.hip", "kvc_calib.hip"):
         o = os.path.join(BUILD, src.replace(".hip", ".o"))
         cmd = [hipcc, "-std=c++17", "-O3", "-fPIC", f"--offload-arch={ARCH}", "-ffp-contract=fast",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -134,8 +134,24 @@ __device__ __forceinline__ float row_sum16(float v) {
 constexpr int kAppThreads = KVC_HEAD_DIM;
 constexpr int kAppMaxTok = 4;
 
-__device__ __forceinline__ void append_unit(const DevSide& s, int side, const uint16_t* __restrict__ x,
-                                            int64_t x_stride, int t0, int n_tok, int u) {
+// Where a call's tokens are: token i of the unit is row i of xu, or row rows[i] (kvc_append_rows).
+struct EveryRow {
+    const uint16_t* __restrict__ xu;
+    __device__ __forceinline__ const uint16_t* at(int i) const { return xu + (int64_t)i * KVC_HEAD_DIM; }
+};
+struct ChosenRows {
+    const uint16_t* __restrict__ xu;
+    const int32_t* __restrict__ rows;
+    int last;  // indices are clamped to [0, last]
+    __device__ __forceinline__ const uint16_t* at(int i) const {
+        const int m = rows[i];
+        return xu + (int64_t)(m < 0 ? 0 : (m > last ? last : m)) * KVC_HEAD_DIM;
+    }
+};
+
+// Tokens x.at(0) .. x.at(n_tok - 1), n_tok <= kAppMaxTok, at positions t0 .. of unit u.
+template <class Rows>
+__device__ __forceinline__ void append_tokens(const DevSide& s, int side, const Rows& x, int t0, int n_tok, int u) {
     __shared__ float xs[kAppMaxTok][KVC_HEAD_DIM];
     __shared__ float red[kAppMaxTok][kAppThreads / 64];
     __shared__ uint8_t cs[kAppMaxTok][KVC_HEAD_DIM];
@@ -145,9 +161,8 @@ __device__ __forceinline__ void append_unit(const DevSide& s, int side, const ui
     const int r = s.r[u], b = s.b[u];
     const float step = s.delta[u];
     const uint16_t* __restrict__ P = s.basis + s.basis_off[u];
-    const uint16_t* __restrict__ xu = x + (int64_t)u * x_stride;
     for (int t = 0; t < n_tok; ++t) {
-        const float v = h2f(xu[(int64_t)t * KVC_HEAD_DIM + i]);
+        const float v = h2f(x.at(t)[i]);
         xs[t][i] = v;
         float s2 = v * v;
         for (int o = 32; o > 0; o >>= 1) s2 += __shfl_xor(s2, o);
@@ -210,7 +225,7 @@ __device__ __forceinline__ void append_unit(const DevSide& s, int side, const ui
                 m &= m - 1;
                 const int il = (i & ~63) + l;
                 const uint16_t* Prow = P + (int64_t)il * KVC_HEAD_DIM;
-                const uint16_t* xrow = xu + (int64_t)t * KVC_HEAD_DIM;
+                const uint16_t* xrow = x.at(t);
                 const uint32_t cl = resolve_code_wave(Prow, Prow, *reinterpret_cast<const uint32_t*>(xrow + 2 * lane), xrow, step,
                                                       1.0 / (double)step, b, sqrtf(pns[il]), xn, lane);
                 if (lane == l) code = cl;
@@ -219,7 +234,6 @@ __device__ __forceinline__ void append_unit(const DevSide& s, int side, const ui
         }
     }
     __syncthreads();
-    if (i >= r) return;
     // Merge, per new token and plane. K: a token's 16 codes of a full coordinate group are 16
     // consecutive slots, i.e. whole 16-bit (p = 1) or 32-bit words that belong to this token alone:
     // the group's lanes OR their fields together and one lane per word stores it. The tail group's
@@ -228,7 +242,7 @@ __device__ __forceinline__ void append_unit(const DevSide& s, int side, const ui
     // One thread owns each coordinate, so the new tokens of a call are written in order.
     uint8_t* __restrict__ stream = s.codes + s.code_off[u];
     const int g16 = r >> 4, rho = r & 15;
-    for (int t = 0; t < n_tok; ++t) {
+    for (int t = 0; t < (i < r ? n_tok : 0); ++t) {
         const int tok = t0 + t, tile = tok / KVC_TILE_TOKENS, tt = tok % KVC_TILE_TOKENS;
         uint8_t* __restrict__ tbase = stream + (int64_t)tile * 8 * r * b;
         const uint32_t c = cs[t][i];
@@ -262,6 +276,11 @@ __device__ __forceinline__ void append_unit(const DevSide& s, int side, const ui
             }
         }
     }
+}
+
+__device__ __forceinline__ void append_unit(const DevSide& s, int side, const uint16_t* __restrict__ x, int64_t x_stride, int t0,
+                                            int n_tok, int u) {
+    append_tokens(s, side, EveryRow{x + (int64_t)u * x_stride}, t0, n_tok, u);
 }
 
 }  // namespace

@@ -260,10 +260,10 @@ __device__ __forceinline__ void pack_v_field(const uint32_t (&c)[4], const uint3
 }
 
 // The tiles of one wavefront: tl = tl0, tl0 + kEncWaves, ... below tl_end (indices into the call's tiles).
-template <int side, int B>
+template <int side, int B, class Rows>
 __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, const float* __restrict__ pnrm, float tol,
                                              float* __restrict__ etok, uint8_t* __restrict__ sb, const uint16_t* __restrict__ Pg,
-                                             uint8_t* __restrict__ stream, const uint16_t* __restrict__ xu, int r, float step,
+                                             uint8_t* __restrict__ stream, const Rows& x, int r, float step,
                                              int t0, int n_tok, int tile_first, int tl0, int tl_end, int lane) {
     const int col = lane & 15, grp = lane >> 4;
     constexpr int h = 1 << (B - 1);
@@ -287,7 +287,7 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
             const int tk = tok0n + 16 * nt + trow;
-            const h8* row = reinterpret_cast<const h8*>(xu + (int64_t)((tk >= lon && tk < hin ? tk : lon) - t0) * kD);
+            const h8* row = reinterpret_cast<const h8*>(x.at((tk >= lon && tk < hin ? tk : lon) - t0));
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) xf[nt][ks] = row[4 * ks + grp];
         }
@@ -427,7 +427,7 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
                             c = 16 * mc + Lcol;
                         }
                         if (tok0 + tkn < lo || tok0 + tkn >= hi) continue;
-                        const uint16_t* xrow = xu + (int64_t)(tok0 + tkn - t0) * kD;
+                        const uint16_t* xrow = x.at(tok0 + tkn - t0);
                         // The token's entries: from its four lanes' fragments by way of LDS, or, once the
                         // fragments hold the next tile, from memory (a load that nothing else would hide).
                         uint32_t xw;
@@ -486,18 +486,16 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
     }
 }
 
-// Block (run of tiles, unit, side): side0 + blockIdx.z (both sides of a kvc_encode_kv in one launch).
-__global__ __launch_bounds__(kEncMmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void encode_mfma_kernel(
-    DevSide ks, DevSide vs, const uint16_t* __restrict__ xk, int64_t xk_stride, const uint16_t* __restrict__ xv,
-    int64_t xv_stride, int side0, int t0, int n_tok, int tile_first, int n_tiles, int tpb) {
+// A block's run of tiles of one unit and side: the basis staged, then a wavefront's tiles each.
+template <class Rows>
+__device__ __forceinline__ void encode_block(const DevSide& s, int side, int u, const Rows& x, int t0, int n_tok, int tile_first,
+                                             int n_tiles, int tpb) {
     extern __shared__ uint8_t esm[];
     uint16_t* Pl = reinterpret_cast<uint16_t*>(esm);          // [128][kPRow] fp16 basis, rows >= r zero
     float* pnrm = reinterpret_cast<float*>(Pl + kD * kPRow);  // [128] ||P_i||
     float* etoks = pnrm + kD;                                 // [waves][64] token norms
     uint8_t* stages = reinterpret_cast<uint8_t*>(etoks + kEncWaves * kTile);  // [waves][kEncStage]
-    const int side = side0 + blockIdx.z;
-    const DevSide& s = side == KVC_SIDE_K ? ks : vs;
-    const int u = blockIdx.y, tid = threadIdx.x;
+    const int tid = threadIdx.x;
     const int r = s.r[u], b = s.b[u];
     const float step = s.delta[u];
     const uint16_t* __restrict__ Pg = s.basis + s.basis_off[u];
@@ -522,17 +520,74 @@ __global__ __launch_bounds__(kEncMmaThreads) __attribute__((amdgpu_waves_per_eu(
     float pmax = fmaxf(pnrm[lane], pnrm[lane + 64]);
     for (int o = 32; o > 0; o >>= 1) pmax = fmaxf(pmax, __shfl_xor(pmax, o));
     const float tol = 33.f * 0x1p-23f * 1.01f * pmax / step;
-    const int64_t xs = side == KVC_SIDE_K ? xk_stride : xv_stride;
-    const uint16_t* __restrict__ xu = (side == KVC_SIDE_K ? xk : xv) + (int64_t)u * xs;
     const int tl0 = blockIdx.x * tpb + wv, tl_end = min((int)(blockIdx.x + 1) * tpb, n_tiles);
     uint8_t* __restrict__ stream = s.codes + s.code_off[u];
     if (side == KVC_SIDE_K) {
-        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_K, B_>(Pl, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, xu, r,
+        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_K, B_>(Pl, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, x, r,
                                                       step, t0, n_tok, tile_first, tl0, tl_end, lane)));
     } else {
-        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_V, B_>(Pl, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, xu, r,
+        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_V, B_>(Pl, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, x, r,
                                                       step, t0, n_tok, tile_first, tl0, tl_end, lane)));
     }
+}
+
+// Block (run of tiles, unit, side): side0 + blockIdx.z (both sides of a kvc_encode_kv in one launch).
+__global__ __launch_bounds__(kEncMmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void encode_mfma_kernel(
+    DevSide ks, DevSide vs, const uint16_t* __restrict__ xk, int64_t xk_stride, const uint16_t* __restrict__ xv,
+    int64_t xv_stride, int side0, int t0, int n_tok, int tile_first, int n_tiles, int tpb) {
+    const int side = side0 + blockIdx.z, u = blockIdx.y;
+    const DevSide& s = side == KVC_SIDE_K ? ks : vs;
+    const int64_t xs = side == KVC_SIDE_K ? xk_stride : xv_stride;
+    encode_block(s, side, u, EveryRow{(side == KVC_SIDE_K ? xk : xv) + (int64_t)u * xs}, t0, n_tok, tile_first, n_tiles, tpb);
+}
+
+// The tokens of kvc_append_rows: rows of xk and xv, positions and counts of each unit.
+struct RowsArgs {
+    const uint16_t* x[2];
+    int64_t stride[2];
+    int n_rows, max_n, cap[2];
+    const int32_t* rows;
+    const int32_t* t0;
+    const int32_t* n;
+};
+
+// Unit u's tokens of one side: *i0 the first whose position is inside [0, capacity), *t its position; returns how many follow.
+__device__ __forceinline__ int rows_range(const RowsArgs& a, int side, int u, int* i0, int* t) {
+    const int64_t t0 = a.t0[u], n = min(max(a.n[u], 0), a.max_n);
+    const int64_t lo = t0 < 0 ? -t0 : 0, hi = min(n, (int64_t)a.cap[side] - t0);
+    if (lo >= hi) return 0;
+    *i0 = (int)lo;
+    *t = (int)(t0 + lo);
+    return (int)(hi - lo);
+}
+
+// Few tokens per unit: block (u, side), kAppMaxTok tokens at a time.
+__global__ __launch_bounds__(kAppThreads) void append_rows_kernel(DevSide ks, DevSide vs, RowsArgs a) {
+    const int u = blockIdx.x, side = blockIdx.y;
+    const DevSide& s = side == KVC_SIDE_K ? ks : vs;
+    const uint16_t* xu = a.x[side] + (int64_t)u * a.stride[side];
+    int i0 = 0, t = 0;
+    const int n = rows_range(a, side, u, &i0, &t);
+    for (int i = 0; i < n; i += kAppMaxTok) {
+        if (i) __syncthreads();  // the codes of the turn before have been read
+        if (a.rows) append_tokens(s, side, ChosenRows{xu, a.rows + (int64_t)u * a.max_n + i0 + i, a.n_rows - 1}, t + i, min(n - i, kAppMaxTok), u);
+        else append_tokens(s, side, EveryRow{xu + (int64_t)(i0 + i) * kD}, t + i, min(n - i, kAppMaxTok), u);
+    }
+}
+
+// Runs of tokens: block (run of tiles, unit, side).
+__global__ __launch_bounds__(kEncMmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void encode_rows_kernel(DevSide ks, DevSide vs,
+                                                                                                                RowsArgs a, int tpb) {
+    const int u = blockIdx.y, side = blockIdx.z;
+    const DevSide& s = side == KVC_SIDE_K ? ks : vs;
+    const uint16_t* xu = a.x[side] + (int64_t)u * a.stride[side];
+    int i0 = 0, t = 0;
+    const int n = rows_range(a, side, u, &i0, &t);
+    if (n == 0) return;
+    const int tile_first = t / kTile, n_tiles = (t + n - 1) / kTile - tile_first + 1;
+    if ((int)blockIdx.x * tpb >= n_tiles) return;
+    if (a.rows) encode_block(s, side, u, ChosenRows{xu, a.rows + (int64_t)u * a.max_n + i0, a.n_rows - 1}, t, n, tile_first, n_tiles, tpb);
+    else encode_block(s, side, u, EveryRow{xu + (int64_t)i0 * kD}, t, n, tile_first, n_tiles, tpb);
 }
 
 // ---------------------------------------------------------------- append
@@ -555,25 +610,34 @@ __global__ __launch_bounds__(kAppThreads) void append_kv_kernel(DevSide k, DevSi
 
 namespace {
 
+// Tiles per block for `units` (unit, side) pairs of n_tiles tiles (whole turns of its wavefronts): the count that
+// minimises rounds of resident blocks (two per CU) x (turns + staging of the basis, about one turn), so that a
+// short run spreads over the chip and a long one stages its basis seldom.
+int encode_tpb(int64_t units, int n_tiles) {
+    const int64_t slots = 2ll * device_cus();
+    int tpb = kEncWaves;
+    int64_t best = -1;
+    for (int turns = 1; turns <= 16; ++turns) {
+        const int64_t blocks = units * ((n_tiles + turns * kEncWaves - 1) / (turns * kEncWaves));
+        const int64_t cost = (blocks + slots - 1) / slots * (turns + 1);
+        if (best < 0 || cost < best) { best = cost; tpb = turns * kEncWaves; }
+    }
+    return tpb;
+}
+
+// Tokens per unit up to which kvc_append_rows takes the few-token kernel.
+constexpr int kRowsAppendMax = 16;
+
+constexpr size_t kEncSmem = (size_t)kD * kPRow * 2 + kD * 4 + kEncWaves * (kTile * 4 + kEncStage);
+
 // Launch of the bulk encoder for `sides` sides of n_units units (side0 the first).
 int launch_encode(const DevSide& k, const DevSide& v, const uint16_t* xk, int64_t xk_stride, const uint16_t* xv, int64_t xv_stride,
                   int side0, int sides, int n_units, int t0, int n_tok, void* stream) {
     const int tile_first = t0 / kTile;
     const int n_tiles = (t0 + n_tok - 1) / kTile - tile_first + 1;
-    // Tiles per block (whole turns of its wavefronts): the count that minimises rounds of resident blocks
-    // (two per CU) x (turns + staging of the basis, about one turn), so that a short run spreads over the
-    // chip and a long one stages its basis seldom.
-    const int64_t slots = 2ll * device_cus();
-    int tpb = kEncWaves;
-    int64_t best = -1;
-    for (int turns = 1; turns <= 16; ++turns) {
-        const int64_t blocks = (int64_t)n_units * sides * ((n_tiles + turns * kEncWaves - 1) / (turns * kEncWaves));
-        const int64_t cost = (blocks + slots - 1) / slots * (turns + 1);
-        if (best < 0 || cost < best) { best = cost; tpb = turns * kEncWaves; }
-    }
-    const size_t smem = (size_t)kD * kPRow * 2 + kD * 4 + kEncWaves * (kTile * 4 + kEncStage);
+    const int tpb = encode_tpb((int64_t)n_units * sides, n_tiles);
     const dim3 grid((n_tiles + tpb - 1) / tpb, n_units, sides);
-    hipLaunchKernelGGL(encode_mfma_kernel, grid, dim3(kEncMmaThreads), smem, (hipStream_t)stream, k, v, xk, xk_stride, xv, xv_stride,
+    hipLaunchKernelGGL(encode_mfma_kernel, grid, dim3(kEncMmaThreads), kEncSmem, (hipStream_t)stream, k, v, xk, xk_stride, xv, xv_stride,
                        side0, t0, n_tok, tile_first, n_tiles, tpb);
     return check_launch("kvc_encode");
 }
@@ -622,4 +686,34 @@ extern "C" int kvc_encode_kv(const kvc_stream_desc* k, const kvc_stream_desc* v,
     hipLaunchKernelGGL(append_kv_kernel, dim3(k->n_units, 2), dim3(kAppThreads), 0, (hipStream_t)stream, dev_side(k),
                        dev_side(v), xk, xk_unit_stride, xv, xv_unit_stride, t0, n_tok);
     return check_launch("kvc_encode_kv");
+}
+
+extern "C" int kvc_append_rows(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* xk, int64_t xk_unit_stride,
+                               const uint16_t* xv, int64_t xv_unit_stride, int32_t n_rows, const int32_t* rows, const int32_t* t0,
+                               const int32_t* n, int32_t max_n, void* stream) {
+    clear_error();
+    if (int e = validate_desc(k, "kvc_append_rows(k)")) return e;
+    if (int e = validate_desc(v, "kvc_append_rows(v)")) return e;
+    if (k->side != KVC_SIDE_K || v->side != KVC_SIDE_V) return set_error(KVC_EINVAL, "kvc_append_rows: descriptor sides");
+    if (k->n_units != v->n_units) return set_error(KVC_EINVAL, "kvc_append_rows: K and V unit counts differ");
+    if (max_n < 0 || n_rows < 0) return set_error(KVC_EINVAL, "kvc_append_rows: negative max_n or n_rows");
+    if (max_n > k->capacity || max_n > v->capacity) return set_error(KVC_ENOSPACE, "kvc_append_rows: max_n > capacity");
+    if (max_n == 0 || k->n_units == 0) return KVC_OK;
+    if (n_rows == 0 || (!rows && max_n > n_rows)) return set_error(KVC_EINVAL, "kvc_append_rows: fewer rows than max_n");
+    if (!t0 || !n) return set_error(KVC_EINVAL, "kvc_append_rows: null pointer");
+    for (const void* p : {(const void*)rows, (const void*)t0, (const void*)n})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return set_error(KVC_EINVAL, "kvc_append_rows: rows, t0 and n must be 4-byte aligned");
+    for (const auto& xs : {std::make_pair(xk, xk_unit_stride), std::make_pair(xv, xv_unit_stride)})
+        if (!xs.first || (reinterpret_cast<uintptr_t>(xs.first) & 15) || (xs.second & 7) || xs.second < (int64_t)n_rows * kD)
+            return set_error(KVC_EINVAL, "kvc_append_rows: xk, xv must be 16-byte aligned with stride a multiple of 8 and >= n_rows*d");
+    const RowsArgs a = {{xk, xv}, {xk_unit_stride, xv_unit_stride}, n_rows, max_n, {k->capacity, v->capacity}, rows, t0, n};
+    if (max_n <= kRowsAppendMax) {
+        hipLaunchKernelGGL(append_rows_kernel, dim3(k->n_units, 2), dim3(kAppThreads), 0, (hipStream_t)stream, dev_side(k), dev_side(v), a);
+    } else {
+        const int n_tiles = (max_n + 2 * kTile - 2) / kTile;  // of the longest run, wherever in a tile it begins
+        const int tpb = encode_tpb(2ll * k->n_units, n_tiles);
+        hipLaunchKernelGGL(encode_rows_kernel, dim3((n_tiles + tpb - 1) / tpb, k->n_units, 2), dim3(kEncMmaThreads), kEncSmem,
+                           (hipStream_t)stream, dev_side(k), dev_side(v), a, tpb);
+    }
+    return check_launch("kvc_append_rows");
 }

@@ -1,0 +1,189 @@
+// kvc_norm_rope on CDNA4 (gfx950): a layer's query, key and value projections become what the cache calls
+// take, in one pass over memory: per-head root-mean-square norm, rotary embedding, rounding to fp16 and the
+// layout by unit.
+//
+// y = x rsqrt(mean_j x_j^2 + eps) w, then pairs (j, j + 64) turned by pos base^(-2j/128). Sixteen lanes take
+// one head: lane c holds elements 4c + [0, 4) and their partners 64 + 4c + [0, 4), so that a rotation pair
+// sits in one lane, the mean is four row rotations, and a head's loads and stores are whole 128-byte lines.
+// A wavefront takes four heads at a time and several turns of them for one token, whose sines and cosines
+// (turns of the angle reduced in fp64, then fp32) it forms once. Statistics and rotation are fp32; the only
+// rounding to fewer bits is the one to fp16 on the way out (the unrotated and the rotated key are both
+// rounded from the fp32 norm, not one from the other).
+//
+// Bound by memory.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "kvc_device.h"
+#include "kvc_internal.h"
+
+namespace kvc {
+namespace {
+
+constexpr int kNrD = KVC_HEAD_DIM;
+constexpr int kNrThreads = 256;
+
+typedef _Float16 nr_h4 __attribute__((ext_vector_type(4)));
+
+struct NrArgs {
+    const void* x[3];        // q, k, v: token-major rows of heads (null: absent)
+    int64_t stride[3];       // elements between tokens
+    int heads[3];            // heads per token: kv_heads G, kv_heads, kv_heads (0: absent)
+    const float* w[3];       // norm weights (null: no norm)
+    uint16_t* out[3];        // q rotated, k unrotated, v (null: not wanted)
+    uint16_t* k_rot;         // k rotated (null: not wanted)
+    const int32_t* pos;
+    float eps;
+    int n_tok, G, kv_heads;
+    int64_t tokens;          // n_seq n_tok
+    int turns;               // turns of four heads per wavefront
+    int waves;               // wavefronts per token
+    int rotate;
+    double freq[kNrD / 2];   // turns per position of each pair
+};
+
+// Four consecutive elements as fp32.
+template <int DT>
+__device__ __forceinline__ float4 load4(const void* p, int64_t at) {
+    if constexpr (DT == KVC_F32) {
+        return *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + at);
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p) + at);
+        if constexpr (DT == KVC_BF16)
+            return float4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                          __uint_as_float(v.y & 0xffff0000u)};
+        else
+            return float4{h2f((uint16_t)v.x), h2f((uint16_t)(v.x >> 16)), h2f((uint16_t)v.y), h2f((uint16_t)(v.y >> 16))};
+    }
+}
+
+// Rounded to nearest even; values past the largest fp16 number become it (the encoder takes finite input).
+__device__ __forceinline__ void store4(uint16_t* p, float4 v) {
+    const float m = 65504.f;
+    const nr_h4 h = {(_Float16)__builtin_amdgcn_fmed3f(v.x, -m, m), (_Float16)__builtin_amdgcn_fmed3f(v.y, -m, m),
+                     (_Float16)__builtin_amdgcn_fmed3f(v.z, -m, m), (_Float16)__builtin_amdgcn_fmed3f(v.w, -m, m)};
+    *reinterpret_cast<nr_h4*>(p) = h;
+}
+
+__device__ __forceinline__ float row_sum16(float v) {
+    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
+    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x124, 0xf, 0xf, true));
+    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x122, 0xf, 0xf, true));
+    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x121, 0xf, 0xf, true));
+    return v;
+}
+
+__device__ __forceinline__ float dot4(float4 a) { return fmaf(a.x, a.x, fmaf(a.y, a.y, fmaf(a.z, a.z, a.w * a.w))); }
+
+template <int DT>
+__global__ __launch_bounds__(kNrThreads) void norm_rope_kernel(const NrArgs a) {
+    const int64_t wave = (int64_t)blockIdx.x * (kNrThreads / 64) + (threadIdx.x >> 6);
+    const int64_t tok = wave / a.waves;
+    if (tok >= a.tokens) return;
+    const int part = (int)(wave - tok * a.waves);
+    const int lane = threadIdx.x & 63, c = lane & 15, grp = lane >> 4;
+    const int64_t seq = tok / a.n_tok, n = tok - seq * a.n_tok;
+    float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.rotate) {
+        const double p = (double)a.pos[tok];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double t = p * a.freq[4 * c + e];
+            sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
+        }
+    }
+    const int total = a.heads[0] + a.heads[1] + a.heads[2];
+    for (int it = 0; it < a.turns; ++it) {
+        const int hh = (part * a.turns + it) * 4 + grp;
+        if (hh >= total) break;
+        const int kind = hh < a.heads[0] ? 0 : (hh < a.heads[0] + a.heads[1] ? 1 : 2);
+        const int h = hh - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
+        const int64_t at = tok * a.stride[kind] + (int64_t)h * kNrD + 4 * c;
+        float4 x = load4<DT>(a.x[kind], at), y = load4<DT>(a.x[kind], at + 64);
+        const float* w = a.w[kind];
+        if (w) {
+            const float ms = row_sum16(dot4(x) + dot4(y)) * (1.f / kNrD);
+            const float s = 1.f / sqrtf(ms + a.eps);
+            const float4 wx = *reinterpret_cast<const float4*>(w + 4 * c), wy = *reinterpret_cast<const float4*>(w + 64 + 4 * c);
+            x = float4{x.x * s * wx.x, x.y * s * wx.y, x.z * s * wx.z, x.w * s * wx.w};
+            y = float4{y.x * s * wy.x, y.y * s * wy.y, y.z * s * wy.z, y.w * s * wy.w};
+        }
+        // unit-major rows: q [unit][token][g], k and v [unit][token]
+        const int g = kind == 0 ? a.G : 1;
+        const int64_t row = ((seq * a.kv_heads + h / g) * a.n_tok + n) * g + h % g;
+        uint16_t* plain = kind == 0 ? nullptr : a.out[kind];
+        uint16_t* turned = kind == 0 ? a.out[0] : (kind == 1 ? a.k_rot : nullptr);
+        if (plain) {
+            store4(plain + row * kNrD + 4 * c, x);
+            store4(plain + row * kNrD + 64 + 4 * c, y);
+        }
+        if (turned) {
+            const float4 u = {x.x * cs[0] - y.x * sn[0], x.y * cs[1] - y.y * sn[1], x.z * cs[2] - y.z * sn[2], x.w * cs[3] - y.w * sn[3]};
+            const float4 v = {x.x * sn[0] + y.x * cs[0], x.y * sn[1] + y.y * cs[1], x.z * sn[2] + y.z * cs[2], x.w * sn[3] + y.w * cs[3]};
+            store4(turned + row * kNrD + 4 * c, u);
+            store4(turned + row * kNrD + 64 + 4 * c, v);
+        }
+    }
+}
+
+}  // namespace
+}  // namespace kvc
+
+using namespace kvc;
+
+extern "C" int kvc_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             int32_t dtype, int32_t n_seq, int32_t n_tok, int32_t kv_heads, int32_t G, const float* wq, const float* wk,
+                             float eps, const int32_t* pos, float rope_base, uint16_t* q_out, uint16_t* k_out, uint16_t* k_rot,
+                             uint16_t* v_out, void* stream) {
+    clear_error();
+    if (dtype != KVC_F16 && dtype != KVC_BF16 && dtype != KVC_F32) return set_error(KVC_EUNSUPPORTED, "kvc_norm_rope: dtype %d", dtype);
+    if (n_seq < 0 || n_tok < 0) return set_error(KVC_EINVAL, "kvc_norm_rope: negative n_seq or n_tok");
+    if (kv_heads < 1 || G < 1 || kv_heads > 65536 || G > 65536 || (int64_t)kv_heads * G > 65536)
+        return set_error(KVC_EINVAL, "kvc_norm_rope: kv_heads = %d, G = %d (at least one, at most 65536 query heads)", kv_heads, G);
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return set_error(KVC_EINVAL, "kvc_norm_rope: eps must be finite and >= 0");
+    if (rope_base != 0.f && (!(rope_base > 1.f) || !std::isfinite(rope_base)))
+        return set_error(KVC_EINVAL, "kvc_norm_rope: rope_base must be 0 (no rotation) or finite and > 1");
+    if ((int64_t)n_seq * n_tok == 0) return KVC_OK;
+    if (!q != !q_out || !v != !v_out || !k != (!k_out && !k_rot))
+        return set_error(KVC_EINVAL, "kvc_norm_rope: an input without its output, or an output without its input");
+    if (!q && !k && !v) return set_error(KVC_EINVAL, "kvc_norm_rope: null pointer");
+    if (rope_base != 0.f && !pos && (q || k_rot)) return set_error(KVC_EINVAL, "kvc_norm_rope: a rotation needs positions");
+    const int size = dtype == KVC_F32 ? 4 : 2, Hq = kv_heads * G;
+    const struct { const void* x; int64_t stride; int heads; } in[3] = {{q, q_stride, Hq}, {k, k_stride, kv_heads}, {v, v_stride, kv_heads}};
+    for (const auto& i : in)
+        if (i.x && ((reinterpret_cast<uintptr_t>(i.x) & 15) || (i.stride * size & 15) || i.stride < (int64_t)i.heads * kNrD))
+            return set_error(KVC_EINVAL, "kvc_norm_rope: inputs must be 16-byte aligned, token strides multiples of 16 bytes and >= a token's heads");
+    for (const void* p : {(const void*)q_out, (const void*)k_out, (const void*)k_rot, (const void*)v_out, (const void*)wq, (const void*)wk})
+        if (reinterpret_cast<uintptr_t>(p) & 15) return set_error(KVC_EINVAL, "kvc_norm_rope: outputs and weights must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(pos) & 3) return set_error(KVC_EINVAL, "kvc_norm_rope: pos must be 4-byte aligned");
+    NrArgs a;
+    a.tokens = (int64_t)n_seq * n_tok;
+    for (int i = 0; i < 3; ++i) {
+        a.x[i] = in[i].x;
+        a.stride[i] = in[i].stride;
+        a.heads[i] = in[i].x ? in[i].heads : 0;
+    }
+    a.w[0] = wq; a.w[1] = wk; a.w[2] = nullptr;
+    a.out[0] = q_out; a.out[1] = k_out; a.out[2] = v_out;
+    a.k_rot = k_rot;
+    a.pos = pos;
+    a.eps = eps;
+    a.n_tok = n_tok;
+    a.G = G;
+    a.kv_heads = kv_heads;
+    a.rotate = rope_base != 0.f;
+    for (int j = 0; j < kNrD / 2; ++j)
+        a.freq[j] = a.rotate ? std::pow((double)rope_base, -2.0 * j / kNrD) / 6.283185307179586476925 : 0.0;
+    const int fours = (a.heads[0] + a.heads[1] + a.heads[2] + 3) / 4;
+    a.turns = fours;
+    a.waves = (fours + a.turns - 1) / a.turns;
+    const int64_t blocks = (a.tokens * a.waves + kNrThreads / 64 - 1) / (kNrThreads / 64);
+    if (blocks > INT32_MAX) return set_error(KVC_EUNSUPPORTED, "kvc_norm_rope: too many tokens");
+    const dim3 grid((unsigned)blocks), blk(kNrThreads);
+    if (dtype == KVC_F16) hipLaunchKernelGGL(norm_rope_kernel<KVC_F16>, grid, blk, 0, (hipStream_t)stream, a);
+    else if (dtype == KVC_BF16) hipLaunchKernelGGL(norm_rope_kernel<KVC_BF16>, grid, blk, 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(norm_rope_kernel<KVC_F32>, grid, blk, 0, (hipStream_t)stream, a);
+    return check_launch("kvc_norm_rope");
+}

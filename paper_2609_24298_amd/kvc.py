@@ -87,6 +87,17 @@ def lib():
         L.kvc_covariance.argtypes = [_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _p, _p]
         L.kvc_eigh.argtypes = [_p, ctypes.c_int32, _p, _p, _p, _p]
         L.kvc_query_variance.argtypes = [_p, _p, ctypes.c_int32, ctypes.c_int32, _p, _p]
+        L.kvc_norm_rope.argtypes = [_p, ctypes.c_int64, _p, ctypes.c_int64, _p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _p, _p, ctypes.c_float, _p,
+                                    ctypes.c_float, _p, _p, _p, _p, _p]
+        L.kvc_tree_attn.argtypes = [ctypes.POINTER(StreamDesc), ctypes.POINTER(StreamDesc), _p, ctypes.c_int32,
+                                    ctypes.c_int32, _p, ctypes.c_int64, _p, ctypes.c_int64, _p, _p, ctypes.c_int32,
+                                    ctypes.c_float, _p, _p, ctypes.c_size_t, _p]
+        L.kvc_tree_attn_workspace.argtypes = [ctypes.POINTER(StreamDesc), ctypes.POINTER(StreamDesc), ctypes.c_int32,
+                                              ctypes.c_int32, ctypes.c_int32]
+        L.kvc_tree_attn_workspace.restype = ctypes.c_size_t
+        L.kvc_append_rows.argtypes = [ctypes.POINTER(StreamDesc), ctypes.POINTER(StreamDesc), _p, ctypes.c_int64, _p,
+                                      ctypes.c_int64, ctypes.c_int32, _p, _p, _p, ctypes.c_int32, _p]
         L.kvc_last_error.restype = ctypes.c_char_p
         L.kvc_version.restype = ctypes.c_int32
         _lib = L
@@ -356,6 +367,96 @@ def kvc_reconstruct(side: Side, t0: int, n_tok: int, out, stream=None):
     assert out.device == side.codes.device
     _check(lib().kvc_reconstruct(ctypes.byref(side.desc), int(t0), int(n_tok), ctypes.c_void_p(out.data_ptr()),
                                  _stream_ptr(stream)))
+
+
+# ------------------------------------------------------------------ verify step of speculative decoding
+
+F16, BF16, F32 = 0, 1, 2  # KVC_F16, KVC_BF16, KVC_F32 of include/kvc.h
+
+
+def _ptr(t):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def kvc_norm_rope(q, k, v, pos, wq, wk, eps: float, rope_base: float, G: int, q_out, k_out, k_rot, v_out, stream=None):
+    """Per-head norm and rotary embedding, laid out by unit. q: (n_seq, n_tok, kv_heads * G * d), k and v:
+    (n_seq, n_tok, kv_heads * d), fp16, bf16 or fp32, each possibly a slice of a wider projection; pos: int32
+    (n_seq, n_tok); wq, wk: f32 (d,) or None (no norm); rope_base 0: no rotation (pos may be None). Outputs fp16:
+    q_out (n_seq * kv_heads, n_tok, G, d), k_out (not rotated), k_rot (rotated) and v_out (n_seq * kv_heads, n_tok, d).
+    An input may be None with its outputs, and either key output."""
+    import torch
+    x0 = next(t for t in (q, k, v) if t is not None)
+    n_seq, n_tok = x0.shape[0], x0.shape[1]
+    kv_heads = q.shape[2] // (G * HEAD_DIM) if q is not None else x0.shape[2] // HEAD_DIM
+    for x, heads in ((q, kv_heads * G), (k, kv_heads), (v, kv_heads)):
+        if x is not None:
+            assert x.dim() == 3 and x.shape == (n_seq, n_tok, heads * HEAD_DIM) and x.dtype == x0.dtype and x.device == x0.device
+            # a dimension of one element has no stride; otherwise one stride between tokens
+            assert x.numel() == 0 or (x.stride(2) == 1 and (n_seq == 1 or n_tok == 1 or x.stride(0) == n_tok * x.stride(1)))
+    for o, n in ((q_out, G), (k_out, 1), (k_rot, 1), (v_out, 1)):
+        if o is not None:
+            assert o.dtype == torch.float16 and o.is_contiguous() and o.device == x0.device
+            assert o.numel() == n_seq * kv_heads * n_tok * n * HEAD_DIM
+    for w in (wq, wk):
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == HEAD_DIM and w.device == x0.device)
+    assert pos is None or (pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_seq * n_tok and pos.device == x0.device)
+    dt = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}[x0.dtype]
+
+    def stride(x):
+        return 0 if x is None else int(x.stride(1) if n_tok > 1 else (x.stride(0) if n_seq > 1 else x.shape[2]))
+
+    _check(lib().kvc_norm_rope(_ptr(q), stride(q), _ptr(k), stride(k), _ptr(v), stride(v), dt, int(n_seq), int(n_tok),
+                               int(kv_heads), int(G), _ptr(wq), _ptr(wk), float(eps), _ptr(pos), float(rope_base),
+                               _ptr(q_out), _ptr(k_out), _ptr(k_rot), _ptr(v_out), _stream_ptr(stream)))
+
+
+def kvc_tree_attn_workspace(k: Side, v: Side, G: int, n_tok: int, max_seq_len: int) -> int:
+    n = lib().kvc_tree_attn_workspace(ctypes.byref(k.desc), ctypes.byref(v.desc), int(G), int(n_tok), int(max_seq_len))
+    if n == 0:
+        _check(KVC_EINVAL)
+    return int(n)
+
+
+def kvc_tree_attn(k: Side, v: Side, q, G: int, xk, xv, mask, seq_len, max_seq_len: int, rope_base: float, out, ws,
+                  stream=None):
+    """Attention of a tree of drafted tokens over the cache and itself. q, out: fp16 (n_units, n_tok, G, d); xk, xv: fp16
+    (n_units, >= n_tok, d), contiguous within a unit; mask: int64 or uint64 (n_units, n_tok), bit m of word n: token n
+    attends to drafted token m; seq_len: int32 (n_units,); rope_base 0: cached keys are not rotated; ws: uint8 workspace."""
+    import torch
+    U, N = k.n_units, q.shape[1]
+    assert q.dim() == 4 and q.shape == (U, N, G, HEAD_DIM) and q.dtype == torch.float16 and q.is_contiguous()
+    assert out.shape == q.shape and out.dtype == torch.float16 and out.is_contiguous()
+    for x in (xk, xv):
+        assert x.dim() == 3 and x.dtype == torch.float16 and x.shape[0] == U and x.shape[1] >= N and x.shape[2] == HEAD_DIM
+        assert (N == 1 or x.stride(1) == HEAD_DIM) and x.stride(2) == 1 and x.device == q.device
+    assert mask.dtype in (torch.int64, torch.uint64) and mask.shape == (U, N) and mask.is_contiguous()
+    assert seq_len.dtype == torch.int32 and seq_len.numel() == U and seq_len.is_contiguous() and v.n_units == U
+    assert q.device == out.device == mask.device == seq_len.device == ws.device == k.codes.device
+    _check(lib().kvc_tree_attn(ctypes.byref(k.desc), ctypes.byref(v.desc), _ptr(q), int(G), int(N), _ptr(xk),
+                               int(xk.stride(0)) if U > 1 else N * HEAD_DIM, _ptr(xv),
+                               int(xv.stride(0)) if U > 1 else N * HEAD_DIM, _ptr(mask), _ptr(seq_len), int(max_seq_len),
+                               float(rope_base), _ptr(out), _ptr(ws), ws.numel(), _stream_ptr(stream)))
+
+
+def kvc_append_rows(k: Side, v: Side, xk, xv, t0, n, rows=None, stream=None):
+    """Append rows of xk, xv (fp16 (n_units, n_rows, d)) to every unit at its own length: unit u's tokens
+    rows[u, 0 .. n[u]) (int32 (n_units, max_n); None: the first n[u] rows) go to positions t0[u] .. of its streams.
+    t0, n: int32 (n_units,)."""
+    import torch
+    U, n_rows = k.n_units, xk.shape[1]
+    for x in (xk, xv):
+        assert x.dim() == 3 and x.dtype == torch.float16 and x.shape == (U, n_rows, HEAD_DIM) and x.device == k.codes.device
+        assert (n_rows <= 1 or x.stride(1) == HEAD_DIM) and x.stride(2) == 1
+    for t in (t0, n):
+        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == U and t.device == xk.device
+    assert rows is None or (rows.dtype == torch.int32 and rows.is_contiguous() and rows.dim() == 2 and rows.shape[0] == U
+                            and rows.device == xk.device)
+    assert v.n_units == U and v.codes.device == xk.device
+    max_n = n_rows if rows is None else rows.shape[1]
+    _check(lib().kvc_append_rows(ctypes.byref(k.desc), ctypes.byref(v.desc), _ptr(xk),
+                                 int(xk.stride(0)) if U > 1 else n_rows * HEAD_DIM, _ptr(xv),
+                                 int(xv.stride(0)) if U > 1 else n_rows * HEAD_DIM, int(n_rows), _ptr(rows), _ptr(t0),
+                                 _ptr(n), int(max_n), _stream_ptr(stream)))
 
 
 def kvc_read_probe(buf, sink, stream=None):
