@@ -14,20 +14,59 @@
 namespace kvc {
 namespace {
 
-constexpr int kTreeWaves = 4;
-constexpr int kTreeThreads = 64 * kTreeWaves;
 constexpr float kTreeShift = 10.f;  // softmax weights are 2^(s - m + 10): fp16 keeps 11 bits of them down to 2^-24 of the largest
 constexpr float kTreeLazy = 5.f;    // the running maximum is raised when a tile beats it by more: weights stay below 2^15
 constexpr int kTreeResync = 32;     // tiles between exact sines and cosines (in between they advance by a rotation)
+
+constexpr float kRawScale = 16777216.f;  // 2^24: a raw code in an fp16 operand is this times too small
+constexpr float kTreeLoScale = 2048.f;  // of the low part of a key
+constexpr int kTreeLoExp = 127 - 11;    // its scale as a matrix operand's exponent
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+// K's low parts (bf8, scaled up) times the queries' leading bits (bf8).
+__device__ __forceinline__ rc_f4 mfma_lo(v8i a, v8i b, rc_f4 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 1, 1, 0, kTreeLoExp, 0, 127);
+}
+// The upper byte of each of a lane's 32 fp16 features: four features of a sixteen per dword, as the keys' low parts lie.
+__device__ __forceinline__ v8i lead_bits(const rc_h8 (&q)[4]) {
+    v8i r;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+        const v4u d = __builtin_bit_cast(v4u, q[ks]);
+        r[2 * ks] = (int)perm(d[1], d[0], 0x07050301u);
+        r[2 * ks + 1] = (int)perm(d[3], d[2], 0x07050301u);
+    }
+    return r;
+}
 
 struct TreeRope {
     double freq[kD / 2];  // turns per position of each pair
 };
 
 struct TreeWork {
-    int M, rows_pb, nrb, n_chunks;  // rows, rows per block, row blocks, chunks per unit
+    int U, M, rows_pb, nrb;  // units, rows of one, rows per block, row blocks
+    int n_blocks;            // blocks that share the tiles of all units (0: no cache at all)
     int max_seq, k_cap_tiles, v_cap_tiles;
 };
+
+// ---------------------------------------------------------------- division of the work
+
+// The tiles of all units, one after another, are cut into equal runs, one for each block: lengths differ between sequences and
+// are known on the device only. The piece of unit u in block b's run leaves its partials in slot b + u, which is unique.
+__device__ __forceinline__ int unit_tokens(const int32_t* __restrict__ seq_len, int u, int max_seq) {
+    const int T = seq_len[u];
+    return T < 0 ? 0 : (T > max_seq ? max_seq : T);
+}
+__device__ __forceinline__ int unit_tiles(const int32_t* __restrict__ seq_len, int u, int max_seq) {
+    return (unit_tokens(seq_len, u, max_seq) + kTile - 1) / kTile;
+}
+__device__ __forceinline__ int64_t run_tiles(int64_t total, int n_blocks) { return (total + n_blocks - 1) / n_blocks; }
+
+__device__ __forceinline__ int64_t wave_total(int64_t v) {
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
 
 // Token of a 16-token quarter in slot (s, e) of the operand that the unpacked value field fills (k_pairs: dword d
 // holds positions d and d + 8), and so of row 4 grp + v of key block tb = 2 s + e / 4, v = e % 4.
@@ -38,137 +77,154 @@ __device__ __forceinline__ int tree_tok(int bv, int tb, int v) {
 
 // ---------------------------------------------------------------- codes of one lane
 
-// The field of one token's coordinate group, 16 codes at slot x of every plane: the dwords that hold it.
-constexpr int tree_k_words(int b) { return b == 8 ? 5 : (b & 4 ? 3 : 0) + (b & 2 ? 2 : 0) + (b & 1 ? 2 : 0); }
-template <int B>
-__device__ __forceinline__ void tree_k_load(const __amdgpu_buffer_rsrc_t rs, int tile_off, int r, uint32_t x, uint32_t (&w)[7]) {
-    int o = 0;
-#pragma unroll
-    for (int k = 0; k < n_planes(B); ++k) {
-        const int P = plane_w(B, k);
-        const int at = tile_off + 8 * r * plane_off(B, k) + (int)((P * x) >> 5) * 4;
-        if (P <= 2) {
-            const v2u v = __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0);
-            w[o] = v[0]; w[o + 1] = v[1];
-            o += 2;
-        } else if (P == 4) {
-            const auto v = __builtin_amdgcn_raw_buffer_load_b96(rs, at, 0, 0);
-            w[o] = v[0]; w[o + 1] = v[1]; w[o + 2] = v[2];
-            o += 3;
-        } else {
-            const v4u v = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0);
-            w[o] = v[0]; w[o + 1] = v[1]; w[o + 2] = v[2]; w[o + 3] = v[3];
-            w[o + 4] = __builtin_amdgcn_raw_buffer_load_b32(rs, at + 16, 0, 0);
-            o += 5;
-        }
-    }
+// A field of sixteen codes is read plane by plane, the planes that a width has chosen by uniform branches (a switch over
+// the widths, compiled eight times, took some fifty registers of the loop around it). w: the 4-bit plane's dwords
+// (or the 8-bit one's first) at 0, the 2-bit one's (or the 8-bit one's rest) at 3, the 1-bit one's at 5.
+constexpr int kFieldWords = 7;
+
+// Byte of the dword in which slot x of each plane begins: of the widest plane (4 or 8 bits), the 2-bit and the 1-bit one.
+struct PlaneAt { int a4, a2, a1; };
+
+// One token's coordinate group, sixteen codes from slot x on of every plane.
+__device__ __forceinline__ PlaneAt tree_k_at(int b, int r, uint32_t x) {
+    PlaneAt p;
+    p.a4 = b == 8 ? (int)(8 * x >> 5) * 4 : (int)(4 * x >> 5) * 4;
+    p.a2 = 8 * r * (b & 4) + (int)(2 * x >> 5) * 4;
+    p.a1 = 8 * r * (b & 6) + (int)(x >> 5) * 4;
+    return p;
 }
-template <int B>
-__device__ __forceinline__ void tree_k_frag(const uint32_t (&w)[7], uint32_t x, uint32_t e512, rc_h8 (&z)[2]) {
-    Fld f[3] = {};
-    int o = 0;
-#pragma unroll
-    for (int k = 0; k < n_planes(B); ++k) {
-        const int P = plane_w(B, k);
-        const uint32_t sh = P * x;  // funnel shifts by its low five bits
-        if (P <= 2) {
-            f[k].w0 = funnel(w[o + 1], w[o], sh);
-            o += 2;
-        } else if (P == 4) {
-            f[k].w0 = funnel(w[o + 1], w[o], sh);
-            f[k].w1 = funnel(w[o + 2], w[o + 1], sh);
-            o += 3;
-        } else {
-            f[k].w0 = funnel(w[o + 1], w[o], sh);
-            f[k].w1 = funnel(w[o + 2], w[o + 1], sh);
-            f[k].w2 = funnel(w[o + 3], w[o + 2], sh);
-            f[k].w3 = funnel(w[o + 4], w[o + 3], sh);
-            o += 5;
-        }
+__device__ __forceinline__ void tree_k_load(const __amdgpu_buffer_rsrc_t rs, int tile_off, int b, const PlaneAt& p, uint32_t (&w)[kFieldWords]) {
+    if (b & 12) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b96(rs, p.a4, tile_off, 0);
+        w[0] = v[0]; w[1] = v[1]; w[2] = v[2];
     }
-    k_pairs<B>(f, false, e512, z);
+    if (b & 8) {
+        const v2u v = __builtin_amdgcn_raw_buffer_load_b64(rs, p.a4 + 12, tile_off, 0);
+        w[3] = v[0]; w[4] = v[1];
+    }
+    if (b & 2) {
+        const v2u v = __builtin_amdgcn_raw_buffer_load_b64(rs, p.a2, tile_off, 0);
+        w[3] = v[0]; w[4] = v[1];
+    }
+    if (b & 1) {
+        const v2u v = __builtin_amdgcn_raw_buffer_load_b64(rs, p.a1, tile_off, 0);
+        w[5] = v[0]; w[6] = v[1];
+    }
 }
 
-// The value field of coordinate 16 n + c, quarter q: 2p bytes per plane.
-template <int B>
-__device__ __forceinline__ void tree_v_load(const __amdgpu_buffer_rsrc_t rs, int tile_off, int r, int n, int c, int q, uint32_t (&w)[4]) {
-    int o = 0;
+// Codes m and m + 8 of a field in the halves of c[m].
+__device__ __forceinline__ void pairs4(uint32_t w0, uint32_t w1, uint32_t (&c)[8]) {
+    const uint32_t y0 = perm(w1, w0, 0x05040100u), y1 = perm(w1, w0, 0x07060302u);
 #pragma unroll
-    for (int k = 0; k < n_planes(B); ++k) {
-        const int P = plane_w(B, k);
-        const int at = tile_off + 8 * r * plane_off(B, k) + v_field_off(P, r, n, c, q);
-        if (P == 1) {
-            w[o] = __builtin_amdgcn_raw_buffer_load_b16(rs, at, 0, 0);
-            o += 1;
-        } else if (P == 2) {
-            w[o] = __builtin_amdgcn_raw_buffer_load_b32(rs, at, 0, 0);
-            o += 1;
-        } else if (P == 4) {
-            const v2u v = __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0);
-            w[o] = v[0]; w[o + 1] = v[1];
-            o += 2;
-        } else {
-            const v4u v = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0);
-            w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3];
-        }
+    for (int m = 0; m < 4; ++m) {
+        c[m] = (y0 >> (4 * m)) & 0x000f000fu;
+        c[m + 4] = (y1 >> (4 * m)) & 0x000f000fu;
     }
 }
-template <int B>
-__device__ __forceinline__ void tree_v_frag(const uint32_t (&w)[4], uint32_t e512, rc_h8 (&z)[2]) {
-    Fld f[3] = {};
-    int o = 0;
+__device__ __forceinline__ void pairs2(uint32_t w, int up, uint32_t (&c)[8]) {
 #pragma unroll
-    for (int k = 0; k < n_planes(B); ++k) {
-        const int P = plane_w(B, k);
-        if (P <= 2) {
-            f[k].w0 = w[o];
-            o += 1;
-        } else if (P == 4) {
-            f[k].w0 = w[o]; f[k].w1 = w[o + 1];
-            o += 2;
-        } else {
-            f[k] = Fld{w[0], w[1], w[2], w[3]};
-        }
+    for (int m = 0; m < 8; ++m) c[m] = (c[m] << up) | ((w >> (2 * m)) & 0x00030003u);
+}
+__device__ __forceinline__ void pairs1(uint32_t w, int up, uint32_t (&c)[8]) {
+    const uint32_t y = perm(0u, w, 0x0c010c00u);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) c[m] = (c[m] << up) | ((y >> m) & 0x00010001u);
+}
+__device__ __forceinline__ void pairs8(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, uint32_t (&c)[8]) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const uint32_t sel = 0x0c040c00u + 0x00010001u * (uint32_t)m;
+        c[m] = perm(w2, w0, sel);
+        c[m + 4] = perm(w3, w1, sel);
     }
-    k_pairs<B>(f, false, e512, z);
+}
+
+// The raw codes of a key field as an operand: the integer c in a half is the fp16 number c 2^-24, which the matrix cores
+// take exactly, so that neither an exponent nor the centring costs an instruction here (both are in the accumulator's
+// start and in the scale of the rotation).
+__device__ __forceinline__ void tree_k_frag(const uint32_t (&w)[kFieldWords], int b, uint32_t x, rc_h8 (&z)[2]) {
+    uint32_t c[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    if (b & 8) {
+        const uint32_t sh = 8 * x;  // funnel shifts by its low five bits
+        pairs8(funnel(w[1], w[0], sh), funnel(w[2], w[1], sh), funnel(w[3], w[2], sh), funnel(w[4], w[3], sh), c);
+    }
+    if (b & 4) pairs4(funnel(w[1], w[0], 4 * x), funnel(w[2], w[1], 4 * x), c);
+    if (b & 2) pairs2(funnel(w[4], w[3], 2 * x), 2, c);
+    if (b & 1) pairs1(funnel(w[6], w[5], x), 1, c);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) z[h] = __builtin_bit_cast(rc_h8, v4u{c[4 * h], c[4 * h + 1], c[4 * h + 2], c[4 * h + 3]});
+}
+
+// The value field of coordinate 16 n + c, quarter q: 2p bytes per plane (words 0, 1 of the 4-bit plane or all four of the
+// 8-bit one, 2 and 3 of the narrow ones).
+__device__ __forceinline__ PlaneAt tree_v_at(int b, int r, int n, int c, int q) {
+    PlaneAt p;
+    p.a4 = b == 8 ? v_field_off(8, r, n, c, q) : v_field_off(4, r, n, c, q);
+    p.a2 = 8 * r * (b & 4) + v_field_off(2, r, n, c, q);
+    p.a1 = 8 * r * (b & 6) + v_field_off(1, r, n, c, q);
+    return p;
+}
+__device__ __forceinline__ void tree_v_load(const __amdgpu_buffer_rsrc_t rs, int tile_off, int b, const PlaneAt& p, uint32_t (&w)[4]) {
+    if (b & 8) {
+        const v4u v = __builtin_amdgcn_raw_buffer_load_b128(rs, p.a4, tile_off, 0);
+        w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3];
+    }
+    if (b & 4) {
+        const v2u v = __builtin_amdgcn_raw_buffer_load_b64(rs, p.a4, tile_off, 0);
+        w[0] = v[0]; w[1] = v[1];
+    }
+    if (b & 2) w[2] = __builtin_amdgcn_raw_buffer_load_b32(rs, p.a2, tile_off, 0);
+    if (b & 1) w[3] = __builtin_amdgcn_raw_buffer_load_b16(rs, p.a1, tile_off, 0);
+}
+// Centred value codes c - 2^(b-1) + 1/2 (exact: 512 + c under fp16's exponent of 512, then one addition). Not left raw like
+// the keys': over a long context the centre's share of the sum would swamp what remains of it.
+__device__ __forceinline__ void tree_v_frag(const uint32_t (&w)[4], int b, rc_h8 (&z)[2]) {
+    uint32_t c[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    if (b & 8) pairs8(w[0], w[1], w[2], w[3], c);
+    if (b & 4) pairs4(w[0], w[1], c);
+    if (b & 2) pairs2(w[2], 2, c);
+    if (b & 1) pairs1(w[3], 1, c);
+    const _Float16 mid = (_Float16)(-512.f - ((float)(1 << (b - 1)) - 0.5f));
+    const rc_h2 mid2 = rc_h2{mid, mid};
+    uint32_t d[8];
+#pragma unroll
+    for (int m = 0; m < 8; ++m) d[m] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(rc_h2, (c[m] << 1) | 0x60006000u) + mid2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) z[h] = __builtin_bit_cast(rc_h8, v4u{d[4 * h], d[4 * h + 1], d[4 * h + 2], d[4 * h + 3]});
 }
 
 // ---------------------------------------------------------------- cached tokens
 
-constexpr int kTreeK = kBtBytes;                     // LDS: P_K^T, then the tile's keys, values, rotation of 64 positions
-constexpr int kTreeV = kTreeK + kTile * kD * 2;
-constexpr int kTreeAdv = kTreeV + kTile * kD * 2;
-constexpr int kTreeSmem = kTreeAdv + (kD / 2) * 8;
+constexpr int kTreeWaves = 8;
+constexpr int kTreeThreads = 64 * kTreeWaves;
+// LDS: P_K^T, the rotation of 64 positions, then two buffers of a tile's keys (fp16), their low parts (bf8) and values (fp16)
+constexpr int kTreeAdv = kBtBytes, kTreeMid = kTreeAdv + (kD / 2) * 8;  // and the centre's share of a rebuilt key
+constexpr int kTreeBuf = kTreeMid + kD * 4;
+constexpr int kBufLo = kTile * kD * 2, kBufV = kBufLo + kTile * kD, kBufBytes = kBufV + kTile * kD * 2;
+constexpr int kTreeSmem = kTreeBuf + 2 * kBufBytes;
 
-// Block: rows [rows_pb rb, ..) of one unit over one of its chunks. Per 64-token tile the wavefronts rebuild and rotate
-// sixteen keys each (K^T = P_K^T Z^T) and unpack the value codes, both to LDS as fp16 operands; then each takes its own
-// 16 CB rows: S^T = K Q^T, the online softmax, O^T += Z_V^T P^T. Key row m of block tb is the token whose value sits in
-// slot (tb, m % 4) of quarter m / 4, so that the lane that computes a weight is the lane whose operand needs it.
-template <int CB, bool ROPE>
-__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_partial_kernel(
-    DevSide K, DevSide V, const uint16_t* __restrict__ q, const int32_t* __restrict__ seq_len, TreeWork wk, TreeRope rope,
-    float* __restrict__ acc_out, float2* __restrict__ ml_out) {
-    const int rb = blockIdx.x % wk.nrb, ch = blockIdx.x / wk.nrb % wk.n_chunks, u = blockIdx.x / wk.nrb / wk.n_chunks;
+// Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, the
+// wavefronts make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
+// (K^T = P_K^T Z^T), rotates them, and unpacks the values of N-tile w, all to LDS in operand order. Wavefront (rw, tw) of RW x
+// 8 / RW then takes rows 16 CB rw .. and the tw-th part of the tile's tokens: S^T = K Q^T, the online softmax, O^T += Z_V^T P^T.
+// Key row m of block tb is the token whose value sits in slot (tb, m % 4) of quarter m / 4, so that the lane that computes
+// a weight is the lane whose operand needs it.
+// A rotated key is fp16 and the rest of it bf8 at 2^11 times its size, met by the queries' leading bits (e5m2 is fp16's upper byte):
+// logits keep about 14 bits of the key for a quarter more matrix work, where fp16 alone would put an error of 2^-12 of
+// each coordinate into the weights.
+template <int CB, int RW, bool ROPE>
+__device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
+                                           const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
+                                           float* __restrict__ acc_out, float2* __restrict__ ml_out) {
+    constexpr int TW = kTreeWaves / RW, TB = TW > 4 ? 1 : 4 / TW;  // token parts, and key blocks of one
     const int tid = threadIdx.x, wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
-    int T = uni(seq_len[u]);
-    T = T < 0 ? 0 : (T > wk.max_seq ? wk.max_seq : T);
-    const int tiles = (T + kTile - 1) / kTile, per = (tiles + wk.n_chunks - 1) / wk.n_chunks;
-    const int tile0 = ch * per, tile1 = min(tiles, tile0 + per);
-    const int row0 = rb * wk.rows_pb + 16 * CB * wv;  // the wavefront's rows
-    const int64_t prow = ((int64_t)u * wk.n_chunks + ch) * wk.M;
-    if (tile0 >= tile1) {
-        if (grp == 0) {
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-                if (row0 + 16 * cb + col < wk.M) ml_out[prow + row0 + 16 * cb + col] = float2{-INFINITY, 0.f};
-        }
-        return;
-    }
+    const int rw = wv % RW, tw = wv / RW;
+    const int row0 = rb * wk.rows_pb + 16 * CB * rw;  // the wavefront's rows
+    const int64_t prow = slot * wk.M;
     const int rk = uni(K.r[u]), bk = uni(K.b[u]), rv = uni(V.r[u]), bv = uni(V.b[u]);
     uint8_t* sm = kvc_dsm;
-    uint8_t* kt = sm + kTreeK;
-    uint8_t* vt = sm + kTreeV;
     float2* adv = reinterpret_cast<float2*>(sm + kTreeAdv);
+    float* mid = reinterpret_cast<float*>(sm + kTreeMid);
     stage_basis_t<KVC_SIDE_K>(sm, K.basis + K.basis_off[u], rk, tid, kTreeThreads);
     if (ROPE && tid < kD / 2) {
         const double t = (double)kTile * rope.freq[tid];
@@ -176,23 +232,28 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2,
         sincospif(2.f * (float)(t - rint(t)), &s, &c);
         adv[tid] = float2{c, s};
     }
-    __syncthreads();
-
     const uint8_t* kstream = uni(K.codes + K.code_off[u]);
     const uint8_t* vstream = uni(V.codes + V.code_off[u]);
     const int ktb = 8 * rk * bk, vtb = 8 * rv * bv;
     const auto krs = __builtin_amdgcn_make_buffer_rsrc((void*)kstream, (short)0, wk.k_cap_tiles * ktb, kRsrcWord3);
     const auto vrs = __builtin_amdgcn_make_buffer_rsrc((void*)vstream, (short)0, wk.v_cap_tiles * vtb, kRsrcWord3);
-    const uint32_t e512 = exp512();
     const int g16 = rk >> 4, rho = rk & 15, nk = (rk + 63) >> 6, nvt = (rv + 15) >> 4;
-    // the lane's key token in the tile, and the slots of its fields
-    const int ktok = 16 * (col >> 2) + tree_tok(bv, wv, col & 3);
+    const int fh = wv & 1, kb = wv >> 1;  // the feature half and token block that the wavefront rebuilds
+    const int ktok = 16 * (col >> 2) + tree_tok(bv, kb, col & 3);
     uint32_t xk[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-        const int cg = 4 * ks + grp;  // a group past the rank reads group 0 (its operand rows of P_K^T are zero)
+        const int cg = 4 * ks + grp;  // a group past the rank reads the first one (its columns of P_K^T are zero)
         xk[ks] = cg < g16 ? (uint32_t)(1024 * cg + 16 * ktok) : (cg == g16 && rho ? (uint32_t)(1024 * g16 + ktok * rho) : (uint32_t)(g16 ? 16 * ktok : rho * ktok));
     }
+    const PlaneAt ka[2] = {tree_k_at(bk, rk, xk[0]), tree_k_at(bk, rk, xk[1])}, va = tree_v_at(bv, rv, wv, col, grp);
+    uint32_t kw[2][kFieldWords], vw[4];
+    auto load = [&](int tile) {
+        tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
+        if (nk > 1) tree_k_load(krs, tile * ktb, bk, ka[1], kw[1]);
+        if (wv < nvt) tree_v_load(vrs, tile * vtb, bv, va, vw);
+    };
+    load(tile0);
     // queries: columns of the operand, features in the order of the rebuilt keys
     rc_h8 qf[CB][4];
 #pragma unroll
@@ -219,124 +280,130 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
     const _Float16 h1 = (_Float16)1.f;
     const rc_h8 ones = {h1, h1, h1, h1, h1, h1, h1, h1};
-    float cs[ROPE ? 4 : 1][4], sn[ROPE ? 4 : 1][4];  // of the lane's pairs 16 rb + 4 grp + v at its token's position
+    float cs[2][4], sn[2][4];  // of the lane's pairs 32 fh + 16 i + 4 grp + v at its token's position, times kRawScale
 
-    uint32_t kw[2][7], vw[2][4];
-    auto load = [&](int tile) {
-        KVC_SWITCH_B(bk, {
-            tree_k_load<B_>(krs, tile * ktb, rk, xk[0], kw[0]);
-            if (nk > 1) tree_k_load<B_>(krs, tile * ktb, rk, xk[1], kw[1]);
-        });
-        KVC_SWITCH_B(bv, {
-            if (wv < nvt) tree_v_load<B_>(vrs, tile * vtb, rv, wv, col, grp, vw[0]);
-            if (wv + 4 < nvt) tree_v_load<B_>(vrs, tile * vtb, rv, wv + 4, col, grp, vw[1]);
-        });
-    };
-    load(tile0);
-#pragma unroll 1
-    for (int tile = tile0; tile < tile1; ++tile) {
-        // ---- keys of the wavefront's sixteen tokens
+    // keys and values of a tile to a buffer; the codes of the tile after it are requested
+    auto make = [&](int tile, uint8_t* buf) {
         if constexpr (ROPE) {
             if ((tile - tile0) % kTreeResync == 0) {
                 const double pos = (double)(tile * kTile + ktok);
+                int p0 = 32 * fh + 4 * grp;
+                asm volatile("" : "+v"(p0));  // opaque: the frequencies are read again, not kept across tiles
 #pragma unroll
-                for (int b4 = 0; b4 < 4; ++b4)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const double t = pos * rope.freq[16 * b4 + 4 * grp + v];
-                        sincospif(2.f * (float)(t - rint(t)), &sn[b4][v], &cs[b4][v]);
+                        const double t = pos * rope.freq[p0 + 16 * i + v];
+                        sincospif(2.f * (float)(t - rint(t)), &sn[i][v], &cs[i][v]);
+                        cs[i][v] *= kRawScale;
+                        sn[i][v] *= kRawScale;
                     }
             } else {
 #pragma unroll
-                for (int b4 = 0; b4 < 4; ++b4)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
-                        const float2 a = adv[16 * b4 + 4 * grp + v];
-                        const float c = cs[b4][v], s = sn[b4][v];
-                        cs[b4][v] = fmaf(c, a.x, -s * a.y);
-                        sn[b4][v] = fmaf(s, a.x, c * a.y);
+                        const float2 a = adv[32 * fh + 16 * i + 4 * grp + v];
+                        const float c = cs[i][v], s = sn[i][v];
+                        cs[i][v] = fmaf(c, a.x, -s * a.y);
+                        sn[i][v] = fmaf(s, a.x, c * a.y);
                     }
             }
         }
-        rc_h8 z[4];
-        KVC_SWITCH_B(bk, {
+        rc_h8 z[4], vz[2];
+        {
             rc_h8 zz[2];
-            tree_k_frag<B_>(kw[0], xk[0], e512, zz);
+            tree_k_frag(kw[0], bk, xk[0], zz);
             z[0] = zz[0];
             z[1] = zz[1];
             if (nk > 1) {
-                tree_k_frag<B_>(kw[1], xk[1], e512, zz);
+                tree_k_frag(kw[1], bk, xk[1], zz);
                 z[2] = zz[0];
                 z[3] = zz[1];
             }
-        });
-        rc_h8 vz[2][2];
-        KVC_SWITCH_B(bv, {
-            tree_v_frag<B_>(vw[0], e512, vz[0]);
-            tree_v_frag<B_>(vw[1], e512, vz[1]);
-        });
-        if (tile + 1 < tile1) load(tile + 1);
-        {
-            const uint8_t* pt = sm + bt_lane(col, grp);
-            rc_h8 lo[2], hi[2];  // rotated features below and above d / 2, matrix steps ks and ks + 2
-#pragma unroll
-            for (int b4 = 0; b4 < 4; ++b4) {
-                rc_f4 a = rc_f4{0.f, 0.f, 0.f, 0.f}, b = a;
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    if (s < 2 || nk > 1) {
-                        a = mfma_h(*reinterpret_cast<const rc_h8*>(pt + bt_block(b4, s)), z[s], a);
-                        b = mfma_h(*reinterpret_cast<const rc_h8*>(pt + bt_block(b4 + 4, s)), z[s], b);
-                    }
-                }
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int e = 4 * (b4 & 1) + v;
-                    if constexpr (ROPE) {
-                        lo[b4 >> 1][e] = (_Float16)fmaf(a[v], cs[b4][v], -b[v] * sn[b4][v]);
-                        hi[b4 >> 1][e] = (_Float16)fmaf(a[v], sn[b4][v], b[v] * cs[b4][v]);
-                    } else {
-                        lo[b4 >> 1][e] = (_Float16)a[v];
-                        hi[b4 >> 1][e] = (_Float16)b[v];
-                    }
-                }
-            }
-            uint8_t* dst = kt + (64 * grp + 16 * wv + col) * 16;
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                *reinterpret_cast<rc_h8*>(dst + 4096 * ks) = lo[ks];
-                *reinterpret_cast<rc_h8*>(dst + 4096 * (ks + 2)) = hi[ks];
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (wv + 4 * i < nvt) {
-                    *reinterpret_cast<rc_h8*>(vt + (wv + 4 * i) * 2048 + lane * 16) = vz[i][0];
-                    *reinterpret_cast<rc_h8*>(vt + (wv + 4 * i) * 2048 + 1024 + lane * 16) = vz[i][1];
-                }
         }
-        __syncthreads();
-        // ---- scores of the wavefront's rows
-        rc_f4 S[4][CB];
+        if (wv < nvt) {
+            tree_v_frag(vw, bv, vz);
+            *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + lane * 16) = vz[0];
+            *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + 1024 + lane * 16) = vz[1];
+        }
+        if (tile + 1 < tile1) load(tile + 1);
+        int po = bt_lane(col, grp) + bt_block(2 * fh, 0);
+        asm volatile("" : "+v"(po));  // opaque: P_K^T is read again for every tile and takes no registers in between
+        const uint8_t* pt = sm + po;
+        rc_f4 a[2], b[2];
 #pragma unroll
-        for (int tb = 0; tb < 4; ++tb)
+        for (int i = 0; i < 2; ++i) {
+            a[i] = *reinterpret_cast<const rc_f4*>(mid + 16 * (2 * fh + i) + 4 * grp);
+            b[i] = *reinterpret_cast<const rc_f4*>(mid + 16 * (2 * fh + i + 4) + 4 * grp);
+        }
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) S[tb][cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < 4; ++s)
+            if (s < 2 || nk > 1)
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
+                for (int i = 0; i < 2; ++i) {
+                    a[i] = mfma_h(*reinterpret_cast<const rc_h8*>(pt + bt_block(i, s)), z[s], a[i]);
+                    b[i] = mfma_h(*reinterpret_cast<const rc_h8*>(pt + bt_block(i + 4, s)), z[s], b[i]);
+                }
+        rc_h8 hx, hy;
+        int lx[2] = {0, 0}, ly[2] = {0, 0};
 #pragma unroll
-            for (int tb = 0; tb < 4; ++tb) {
-                const rc_h8 kf = *reinterpret_cast<const rc_h8*>(kt + (256 * ks + 64 * grp + 16 * tb + col) * 16);
+        for (int i = 0; i < 2; ++i) {
+            float x[4], y[4];
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) S[tb][cb] = mfma_h(kf, qf[cb][ks], S[tb][cb]);
+            for (int v = 0; v < 4; ++v) {
+                x[v] = ROPE ? fmaf(a[i][v], cs[i][v], -b[i][v] * sn[i][v]) : a[i][v] * kRawScale;
+                y[v] = ROPE ? fmaf(a[i][v], sn[i][v], b[i][v] * cs[i][v]) : b[i][v] * kRawScale;
+                hx[4 * i + v] = (_Float16)x[v];
+                hy[4 * i + v] = (_Float16)y[v];
+                x[v] = (x[v] - (float)hx[4 * i + v]) * kTreeLoScale;
+                y[v] = (y[v] - (float)hy[4 * i + v]) * kTreeLoScale;
             }
-        if ((tile + 1) * kTile > T) {  // the context's last tile
+            lx[i] = __builtin_amdgcn_cvt_pk_bf8_f32(x[0], x[1], lx[i], false);
+            lx[i] = __builtin_amdgcn_cvt_pk_bf8_f32(x[2], x[3], lx[i], true);
+            ly[i] = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], ly[i], false);
+            ly[i] = __builtin_amdgcn_cvt_pk_bf8_f32(y[2], y[3], ly[i], true);
+        }
+        uint8_t* dst = buf + (64 * grp + 16 * kb + col) * 16;
+        *reinterpret_cast<rc_h8*>(dst + 4096 * fh) = hx;
+        *reinterpret_cast<rc_h8*>(dst + 4096 * (fh + 2)) = hy;
+        *reinterpret_cast<int2*>(dst + kBufLo + 8 * fh) = int2{lx[0], lx[1]};
+        *reinterpret_cast<int2*>(dst + kBufLo + 4096 + 8 * fh) = int2{ly[0], ly[1]};
+    };
+    // the wavefront's rows against its tokens of a tile
+    auto attend = [&](int tile, const uint8_t* buf) {
+        // opaque, so that the leading bits are formed again for every tile and take no registers in between
 #pragma unroll
-            for (int tb = 0; tb < 4; ++tb)
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(qf[cb][ks]));
+        const int tb0 = TB * tw;  // first key block of the wavefront's tokens
+        // ---- scores
+        rc_f4 S[TB][CB];
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            const uint8_t* kr = buf + (64 * grp + 16 * (tb0 + t) + col) * 16;
+            const v4i l0 = *reinterpret_cast<const v4i*>(kr + kBufLo), l1 = *reinterpret_cast<const v4i*>(kr + kBufLo + 4096);
+            const v8i lo = {l0[0], l0[1], l0[2], l0[3], l1[0], l1[1], l1[2], l1[3]};
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_lo(lo, lead_bits(qf[cb]), rc_f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const rc_h8 kf = *reinterpret_cast<const rc_h8*>(kr + 4096 * ks);
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_h(kf, qf[cb][ks], S[t][cb]);
+            }
+        }
+        if ((tile + 1) * kTile > T) {  // the context's last tile
+            int bvo = bv;
+            asm volatile("" : "+s"(bvo));  // opaque: the tokens of the lane's rows are not kept across tiles
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    if (tile * kTile + 16 * grp + tree_tok(bv, tb, v) >= T)
+                    if (tile * kTile + 16 * grp + tree_tok(bvo, tb0 + t, v) >= T)
 #pragma unroll
-                        for (int cb = 0; cb < CB; ++cb) S[tb][cb][v] = -INFINITY;
+                        for (int cb = 0; cb < CB; ++cb) S[t][cb][v] = -INFINITY;
         }
         // ---- online softmax
         float top[CB];
@@ -345,9 +412,9 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2,
         for (int cb = 0; cb < CB; ++cb) {
             top[cb] = S[0][cb][0];
 #pragma unroll
-            for (int tb = 0; tb < 4; ++tb)
+            for (int t = 0; t < TB; ++t)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) top[cb] = fmaxf(top[cb], S[tb][cb][v]);
+                for (int v = 0; v < 4; ++v) top[cb] = fmaxf(top[cb], S[t][cb][v]);
             raise = raise || top[cb] > m[cb] + lazy;
         }
         if (__any(raise)) {
@@ -356,52 +423,165 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2,
                 float t = fmaxf(top[cb], __shfl_xor(top[cb], 16));
                 t = fmaxf(t, __shfl_xor(t, 32));
                 if (t > m[cb]) {
-                    const float a = __builtin_amdgcn_exp2f((m[cb] - t) * qs);
+                    const float al = __builtin_amdgcn_exp2f((m[cb] - t) * qs);
                     m[cb] = t;
-                    L[cb] *= a;
+                    L[cb] *= al;
 #pragma unroll
-                    for (int n = 0; n < 8; ++n) O[n][cb] *= a;
+                    for (int n = 0; n < 8; ++n) O[n][cb] *= al;
                 }
             }
         }
-        rc_h8 P[2][CB];
+        // a row that has seen no token yet (a part of a short last tile) has every weight 0
+        rc_h8 P[TB > 1 ? TB / 2 : 1][CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            const float off = fmaf(-m[cb], qs, kTreeShift);
+            const float off = m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs, kTreeShift);
+            if constexpr (TB == 1) P[0][cb] = rc_h8{};
 #pragma unroll
-            for (int tb = 0; tb < 4; ++tb)
+            for (int t = 0; t < TB; ++t)
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    P[tb >> 1][cb][4 * (tb & 1) + v] = (_Float16)__builtin_amdgcn_exp2f(fmaf(S[tb][cb][v], qs, off));
+                for (int v = 0; v < 4; ++v) {
+                    const _Float16 p = (_Float16)__builtin_amdgcn_exp2f(fmaf(S[t][cb][v], qs, off));
+                    if constexpr (TB > 1) P[t >> 1][cb][4 * (t & 1) + v] = p;
+                    else P[0][cb][v] = p;
+                }
+            if constexpr (TB == 1)
+                if (tb0 & 1) P[0][cb] = __builtin_shufflevector(P[0][cb], P[0][cb], 4, 5, 6, 7, 0, 1, 2, 3);
         }
         // ---- values
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < (TB > 1 ? TB / 2 : 1); ++s) {
+            const uint8_t* vr = buf + kBufV + ((tb0 >> 1) + s) * 1024 + lane * 16;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[s][cb], L[cb]);
 #pragma unroll
             for (int n = 0; n < 8; ++n)
                 if (n < nvt) {
-                    const rc_h8 vf = *reinterpret_cast<const rc_h8*>(vt + n * 2048 + s * 1024 + lane * 16);
+                    const rc_h8 vf = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf, P[s][cb], O[n][cb]);
                 }
         }
-        __syncthreads();
-    }
+    };
+    __syncthreads();  // P_K^T
+    {   // the centre's share of a key, -(2^(b-1) - 1/2) sum_i P_i: features 16 wv + 4 grp + v, in every column
+        const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
+        const rc_h8 cc = {c, c, c, c, c, c, c, c};
+        rc_f4 a = rc_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        const int row = row0 + 16 * cb + col;
-        if (row >= wk.M) continue;
-        if (grp == 0) ml_out[prow + row] = float2{fmaf(m[cb], qs, -kTreeShift), L[cb][0]};
+        for (int s = 0; s < 4; ++s) a = mfma_h(*reinterpret_cast<const rc_h8*>(sm + bt_block(wv, s) + bt_lane(col, grp)), cc, a);
+        if (col == 0) *reinterpret_cast<rc_f4*>(mid + 16 * wv + 4 * grp) = a * (1.f / kRawScale);
+    }
+    __syncthreads();
+    const bool late = wv >= kTreeWaves / 2;
+#pragma unroll 1
+    for (int tile = tile0 - 1; tile < tile1; ++tile) {
+        // One wavefront of each SIMD makes the next tile and then attends to the current one, the other (late) the other way
+        // round, so that the matrix and vector work of the two overlap: the late ones meet the barrier between the two.
+        if (tile + 1 < tile1) make(tile + 1, sm + kTreeBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
+        if (late) __syncthreads();
+        const int at = late ? tile + 1 : tile;
+        if (at >= tile0 && at < tile1 && (TW <= 4 || tw < 4)) attend(at, sm + kTreeBuf + ((at - tile0) & 1) * kBufBytes);
+        if (!late) __syncthreads();
+    }
+    if constexpr (TW == 1) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const int row = row0 + 16 * cb + col;
+            if (row >= wk.M) continue;
+            if (grp == 0) ml_out[prow + row] = float2{fmaf(m[cb], qs, -kTreeShift), L[cb][0]};
+#pragma unroll
+            for (int n = 0; n < 8; ++n)
+                if (n < nvt) *reinterpret_cast<rc_f4*>(acc_out + (prow + row) * kD + 16 * n + 4 * grp) = O[n][cb];
+        }
+    } else {  // the token parts meet in LDS (the tiles' buffers)
+        static_assert(CB == 1, "token parts have sixteen rows a wavefront");
+        constexpr int kPitch = kD + 4;
+        float* parts = reinterpret_cast<float*>(sm + kTreeBuf);             // [TW][16 RW][kPitch]
+        float* tops = parts + kTreeWaves * 16 * kPitch;                     // [TW][16 RW]
+        float* sums = tops + kTreeWaves * 16;                               // [TW][16 RW]
+        static_assert((kTreeWaves * 16 * (kPitch + 2)) * 4 <= 2 * kBufBytes, "parts exceed the buffers");
+        __syncthreads();  // the late wavefronts have read their last tile
+        if (grp == 0) tops[16 * wv + col] = m[0];  // wavefronts are in the order (tw, rw)
+        __syncthreads();
+        float t = tops[16 * rw + col];
+#pragma unroll
+        for (int i = 1; i < TW; ++i) t = fmaxf(t, tops[16 * (RW * i + rw) + col]);
+        const float al = m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[0] - t) * qs);
+        if (grp == 0) sums[16 * wv + col] = al * L[0][0];
 #pragma unroll
         for (int n = 0; n < 8; ++n)
-            if (n < nvt) *reinterpret_cast<rc_f4*>(acc_out + (prow + row) * kD + 16 * n + 4 * grp) = O[n][cb];
+            if (n < nvt) *reinterpret_cast<rc_f4*>(parts + (16 * wv + col) * kPitch + 16 * n + 4 * grp) = O[n][0] * al;
+        __syncthreads();
+        if (tw == 0 && grp == 0 && row0 + col < wk.M) {
+            float l = sums[16 * rw + col];
+#pragma unroll
+            for (int i = 1; i < TW; ++i) l += sums[16 * (RW * i + rw) + col];
+            ml_out[prow + row0 + col] = float2{fmaf(t, qs, -kTreeShift), l};
+        }
+        for (int e = tid; e < 16 * RW * (kD / 4); e += kTreeThreads) {
+            const int r = e / (kD / 4), c4 = e % (kD / 4) * 4;
+            const int row = rb * wk.rows_pb + r;
+            if (c4 >= 16 * nvt || row >= wk.M) continue;
+            rc_f4 x = *reinterpret_cast<const rc_f4*>(parts + r * kPitch + c4);
+#pragma unroll
+            for (int i = 1; i < TW; ++i) x += *reinterpret_cast<const rc_f4*>(parts + (16 * RW * i + r) * kPitch + c4);
+            *reinterpret_cast<rc_f4*>(acc_out + (prow + row) * kD + c4) = x;
+        }
+    }
+}
+
+template <int CB, int RW, bool ROPE>
+__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_partial_kernel(
+    DevSide K, DevSide V, const uint16_t* __restrict__ q, const int32_t* __restrict__ seq_len, TreeWork wk, TreeRope rope,
+    float* __restrict__ acc_out, float2* __restrict__ ml_out) {
+    const int rb = blockIdx.x % wk.nrb, b = blockIdx.x / wk.nrb;
+    const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6);
+    // the block's run of tiles and where it begins: a thread counts the tiles of some consecutive units
+    int64_t* waves = reinterpret_cast<int64_t*>(kvc_dsm);  // [8] tiles of each wavefront's units, then the first unit and tile
+    const int cu = (wk.U + kTreeThreads - 1) / kTreeThreads, u_lo = min(wk.U, tid * cu), u_hi = min(wk.U, u_lo + cu);
+    int64_t mine = 0;
+    for (int i = u_lo; i < u_hi; ++i) mine += unit_tiles(seq_len, i, wk.max_seq);
+    int64_t upto = mine;  // within the wavefront
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 63) waves[wv] = upto;
+    __syncthreads();
+    int64_t total = 0, before = upto - mine;
+    for (int i = 0; i < kTreeWaves; ++i) {
+        if (i < wv) before += waves[i];
+        total += waves[i];
+    }
+    const int64_t per = run_tiles(total, wk.n_blocks);
+    int64_t g = per * b;
+    const int64_t g1 = min(total, g + per);
+    if (g >= g1) return;
+    if (g >= before && g < before + mine) {
+        int u = u_lo;
+        int64_t at = before;
+        for (int n; at + (n = unit_tiles(seq_len, u, wk.max_seq)) <= g; ++u) at += n;
+        waves[kTreeWaves] = u;
+        waves[kTreeWaves + 1] = g - at;
+    }
+    __syncthreads();
+    int u = uni((int)waves[kTreeWaves]), t0 = uni((int)waves[kTreeWaves + 1]);
+    int left = uni((int)(g1 - g));
+#pragma unroll 1
+    for (; left > 0; ++u, t0 = 0) {
+        const int T = uni(unit_tokens(seq_len, u, wk.max_seq)), tiles = (T + kTile - 1) / kTile;
+        const int t1 = min(tiles, t0 + left);
+        if (t1 <= t0) continue;
+        left -= t1 - t0;
+        __syncthreads();  // LDS of the piece before, or of the count above, has been read
+        tree_piece<CB, RW, ROPE>(K, V, q, wk, rope, u, T, t0, t1, rb, (int64_t)b + u, acc_out, ml_out);
     }
 }
 
 // ---------------------------------------------------------------- drafted tokens, merge, output
 
+constexpr int kFinThreads = 256;
 constexpr int kFinRows = 16;
 constexpr int kFinZ = kBtBytes;                              // LDS: P_V^T, then z [16][132] f32
 constexpr int kFinZPitch = kD + 4;
@@ -410,18 +590,23 @@ constexpr int kFinXPitch = kD + 8;
 constexpr int kFinP = kFinX + KVC_TREE_MAX_TOKENS * kFinXPitch * 2;  // weights [16][72] fp16
 constexpr int kFinPPitch = KVC_TREE_MAX_TOKENS + 8;
 constexpr int kFinRed = kFinP + kFinRows * kFinPPitch * 2;   // maxima and sums of the wavefronts [2][4][16], row maxima [16], 1 / sums [16]
-constexpr int kFinSmem = kFinRed + (2 * 4 * 16 + 32) * 4;
+constexpr int kFinCount = kFinRed + (2 * 4 * 16 + 32) * 4;    // [8] tiles
+constexpr int kFinSmem = kFinCount + 8 * 8;
+static_assert(kFinSmem <= 64 * 1024, "no attribute is set for it");
 
-// Block: sixteen rows of one unit. z = sum_c acc_c 2^(m_c - M) over the chunks, the drafted tokens' weights 2^(s - M),
-// out = (step_V P_V^T z + sum_m p_m xv_m) / l.
-__global__ __launch_bounds__(kTreeThreads) void tree_finish_kernel(DevSide V, const uint16_t* __restrict__ q, int G, int n_tok,
-                                                                   const uint16_t* __restrict__ xk, int64_t xk_stride,
-                                                                   const uint16_t* __restrict__ xv, int64_t xv_stride,
-                                                                   const uint64_t* __restrict__ mask, TreeWork wk,
-                                                                   const float* __restrict__ acc, const float2* __restrict__ ml,
-                                                                   uint16_t* __restrict__ out) {
-    const int nfb = (wk.M + kFinRows - 1) / kFinRows;
-    const int u = blockIdx.x / nfb, row0 = blockIdx.x % nfb * kFinRows;
+// Block: R rows of one unit (columns of the products past R repeat the last row). z = sum_c acc_c 2^(m_c - M) over the unit's
+// pieces, the drafted tokens' weights 2^(s - M), out = (step_V P_V^T z + sum_m p_m xv_m) / l. With few rows in all, blocks
+// of four rows, whose threads also share the pieces.
+template <int R>
+__global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, const uint16_t* __restrict__ q, int G, int n_tok,
+                                                                  const uint16_t* __restrict__ xk, int64_t xk_stride,
+                                                                  const uint16_t* __restrict__ xv, int64_t xv_stride,
+                                                                  const uint64_t* __restrict__ mask, const int32_t* __restrict__ seq_len,
+                                                                  TreeWork wk, const float* __restrict__ acc, const float2* __restrict__ ml,
+                                                                  uint16_t* __restrict__ out) {
+    constexpr int CG = 16 / R;  // threads of a row: CG x 16, eight coordinates each, every CG-th piece
+    const int nfb = (wk.M + R - 1) / R;
+    const int u = blockIdx.x / nfb, row0 = blockIdx.x % nfb * R;
     const int tid = threadIdx.x, wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
     uint8_t* sm = kvc_dsm;
     float* zs = reinterpret_cast<float*>(sm + kFinZ);
@@ -430,15 +615,29 @@ __global__ __launch_bounds__(kTreeThreads) void tree_finish_kernel(DevSide V, co
     float* red = reinterpret_cast<float*>(sm + kFinRed);
     float* big = red + 2 * 4 * 16;
     float* inv = big + 16;
+    int64_t* count = reinterpret_cast<int64_t*>(sm + kFinCount);  // tiles of all units and of those before u, by wavefront
     const int rv = uni(V.r[u]);
-    const int row = min(row0 + col, wk.M - 1);
+    const int row = min(row0 + min(col, R - 1), wk.M - 1);
     const uint64_t live = n_tok == 64 ? ~0ull : (1ull << n_tok) - 1ull;
     const uint64_t mine = mask[(int64_t)u * n_tok + row / G] & live;
-    if (wk.n_chunks > 0) stage_basis_t<KVC_SIDE_K>(sm, V.basis + V.basis_off[u], rv, tid, kTreeThreads);
+    int tiles = 0;
+    if (wk.n_blocks > 0) {
+        tiles = uni(unit_tiles(seq_len, u, wk.max_seq));
+        int64_t all = 0, before = 0;
+        for (int i = tid; i < wk.U; i += kFinThreads) {
+            const int n = unit_tiles(seq_len, i, wk.max_seq);
+            all += n;
+            if (i < u) before += n;
+        }
+        all = wave_total(all);
+        before = wave_total(before);
+        if (lane == 0) { count[wv] = all; count[4 + wv] = before; }
+        if (tiles) stage_basis_t<KVC_SIDE_K>(sm, V.basis + V.basis_off[u], rv, tid, kFinThreads);
+    }
     // drafted tokens that some row of the unit names
     uint64_t named = lane < n_tok ? mask[(int64_t)u * n_tok + lane] & live : 0ull;
     for (int o = 1; o < 64; o <<= 1) named |= __shfl_xor(named, o);
-    for (int e = tid; e < KVC_TREE_MAX_TOKENS * (kD / 8); e += kTreeThreads) {
+    for (int e = tid; e < KVC_TREE_MAX_TOKENS * (kD / 8); e += kFinThreads) {
         const int t = e >> 4, c8 = e & 15;
         uint4 v = {0u, 0u, 0u, 0u};
         if ((named >> t) & 1) v = *reinterpret_cast<const uint4*>(xv + (int64_t)u * xv_stride + (int64_t)t * kD + 8 * c8);
@@ -467,36 +666,57 @@ __global__ __launch_bounds__(kTreeThreads) void tree_finish_kernel(DevSide V, co
     top = fmaxf(top, __shfl_xor(top, 32));
     if (grp == 0) red[wv * 16 + col] = top;
     __syncthreads();
-    // row r's sixteen threads: maxima and sums over the chunks
-    const int mr = tid >> 4, mc = tid & 15;
+    // the threads of row mr: maxima and sums over the pieces, whose slots follow one another
+    const int mr = tid / (16 * CG), mi = tid % (16 * CG), mc = mi & 15, cg = mi >> 4;
     const int mrow = min(row0 + mr, wk.M - 1);
+    int64_t slot0 = 0;
+    int n_pieces = 0;
+    if (tiles) {
+        const int64_t before = (count[4] + count[5]) + (count[6] + count[7]);
+        const int64_t per = run_tiles((count[0] + count[1]) + (count[2] + count[3]), wk.n_blocks);
+        const int64_t b0 = before / per;
+        slot0 = b0 + u;
+        n_pieces = (int)((before + tiles - 1) / per - b0) + 1;
+    }
+    const float2* mlr = ml + slot0 * wk.M + mrow;
     float M = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
-    for (int c = 0; c < wk.n_chunks; ++c) M = fmaxf(M, ml[((int64_t)u * wk.n_chunks + c) * wk.M + mrow].x);
+    for (int c = mi; c < n_pieces; c += 16 * CG) M = fmaxf(M, mlr[(int64_t)c * wk.M].x);
+#pragma unroll
+    for (int o = 1; o < 16 * CG; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
     const float Mf = M == -INFINITY ? 0.f : M;
     float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
-    for (int c = 0; c < wk.n_chunks; ++c) {
-        const int64_t pr = ((int64_t)u * wk.n_chunks + c) * wk.M + mrow;
-        const float2 v = ml[pr];
-        if (v.x == -INFINITY) continue;  // an empty chunk has no accumulators
-        const float w = __builtin_amdgcn_exp2f(v.x - Mf);
-        l = fmaf(w, v.y, l);
-        if (8 * mc < ((rv + 15) & ~15)) {
-            const float4 a = *reinterpret_cast<const float4*>(acc + pr * kD + 8 * mc), b = *reinterpret_cast<const float4*>(acc + pr * kD + 8 * mc + 4);
+    {
+        const bool have = 8 * mc < ((rv + 15) & ~15);
+        const float* ar = acc + (slot0 * wk.M + mrow) * kD + (have ? 8 * mc : 0);
+        const int64_t stride = (int64_t)wk.M * kD;
+#pragma unroll 4
+        for (int c = cg; c < n_pieces; c += CG) {
+            const float2 v = mlr[(int64_t)c * wk.M];
+            const float4 a = *reinterpret_cast<const float4*>(ar + c * stride), b = *reinterpret_cast<const float4*>(ar + c * stride + 4);
+            const float w = __builtin_amdgcn_exp2f(v.x - Mf);
+            l = fmaf(w, v.y, l);
             z[0] = fmaf(w, a.x, z[0]); z[1] = fmaf(w, a.y, z[1]); z[2] = fmaf(w, a.z, z[2]); z[3] = fmaf(w, a.w, z[3]);
             z[4] = fmaf(w, b.x, z[4]); z[5] = fmaf(w, b.y, z[5]); z[6] = fmaf(w, b.z, z[6]); z[7] = fmaf(w, b.w, z[7]);
         }
+#pragma unroll
+        for (int o = 16; o < 16 * CG; o <<= 1) {
+            l += __shfl_xor(l, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] += __shfl_xor(z[e], o);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
     }
-    if (mc == 0) big[mr] = Mf;
+    if (mi == 0) big[mr] = Mf;
     __syncthreads();
     {
-        const float Mc = big[col];
-        float p[4], sum = 0.f;
+        const float Mc = big[min(col, R - 1)];
+        float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const _Float16 h = (_Float16)__builtin_amdgcn_exp2f(s[v] - Mc);
             ps[col * kFinPPitch + 16 * wv + 4 * grp + v] = h;
-            p[v] = (float)h;
-            sum += p[v];
+            sum += (float)h;
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
@@ -506,24 +726,26 @@ __global__ __launch_bounds__(kTreeThreads) void tree_finish_kernel(DevSide V, co
     {
         const float sum = l + ((red[64 + mr] + red[80 + mr]) + (red[96 + mr] + red[112 + mr]));
         const float i = sum > 0.f ? 1.f / sum : 0.f;
-        if (mc == 0) inv[mr] = i;
+        if (mi == 0) inv[mr] = i;
+        if (cg == 0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) zs[mr * kFinZPitch + 8 * mc + e] = z[e] * i;
+            for (int e = 0; e < 8; ++e) zs[mr * kFinZPitch + 8 * mc + e] = z[e] * i;
     }
     __syncthreads();
-    const float step = V.delta[u], rinv = inv[col];
+    const int zc = min(col, R - 1);
+    const float step = V.delta[u], rinv = inv[zc];
     rc_f4 o[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int rb = 2 * wv + i;
         rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f}, t = c;
-        if (wk.n_chunks > 0) {
+        if (tiles) {
 #pragma unroll
             for (int st = 0; st < 4; ++st) {
                 rc_h8 hi, lo;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float x = zs[col * kFinZPitch + bt_coord<KVC_SIDE_K>(32 * st) + 16 * grp + (e >> 1) + 8 * (e & 1)];
+                    const float x = zs[zc * kFinZPitch + bt_coord<KVC_SIDE_K>(32 * st) + 16 * grp + (e >> 1) + 8 * (e & 1)];
                     const _Float16 h = (_Float16)x;
                     hi[e] = h;
                     lo[e] = (_Float16)(x - (float)h);
@@ -544,7 +766,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_finish_kernel(DevSide V, co
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[i][v] = fmaf(c[v], step, t[v] * rinv);
     }
-    if (row0 + col < wk.M) {
+    if (col < R && row0 + col < wk.M) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             typedef _Float16 h4 __attribute__((ext_vector_type(4)));
@@ -556,11 +778,9 @@ __global__ __launch_bounds__(kTreeThreads) void tree_finish_kernel(DevSide V, co
 
 // ---------------------------------------------------------------- host side
 
-constexpr int kTreeMaxChunks = 128;
-
 struct TreeLayout {
     TreeWork wk;
-    int cb;
+    int cb, rw;
     int64_t acc, ml, total;
 };
 
@@ -568,29 +788,40 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     TreeLayout t;
     const int U = k->n_units, tiles = (max_seq + kTile - 1) / kTile;
     t.wk.M = n_tok * G;
-    t.cb = t.wk.M <= 64 ? 1 : 2;
-    t.wk.rows_pb = 64 * t.cb;
+    t.cb = t.wk.M <= 128 ? 1 : 2;
+    t.rw = t.wk.M <= 32 ? 2 : (t.wk.M <= 64 ? 4 : 8);
+    t.wk.rows_pb = 16 * t.cb * t.rw;
     t.wk.nrb = (t.wk.M + t.wk.rows_pb - 1) / t.wk.rows_pb;
     t.wk.max_seq = max_seq;
     t.wk.k_cap_tiles = (k->capacity + kTile - 1) / kTile;
     t.wk.v_cap_tiles = (v->capacity + kTile - 1) / kTile;
-    // Chunks per unit: the count that minimises rounds of resident blocks (two per CU) x (tiles + set-up, about
-    // three tiles) and the merge, which reads every chunk of every row.
-    const int64_t slots = 2ll * device_cus();
-    t.wk.n_chunks = 0;
-    double best = -1.0;
-    for (int n = 1; n <= std::min(tiles, kTreeMaxChunks); ++n) {
-        const int per = (tiles + n - 1) / n;
-        const int64_t blocks = (int64_t)U * t.wk.nrb * n;
-        const double cost = (double)((blocks + slots - 1) / slots) * (per + 3.0) + 0.1 * n;
-        if (best < 0.0 || cost < best) { best = cost; t.wk.n_chunks = n; }
-    }
-    const int64_t rows = (int64_t)U * t.wk.n_chunks * t.wk.M;
+    // One block for every CU (its LDS lets no second one in), as long as there are tiles for them.
+    t.wk.U = U;
+    t.wk.n_blocks = (int)std::min<int64_t>(std::max(1, device_cus() / t.wk.nrb), (int64_t)U * tiles);
+    const int64_t rows = t.wk.n_blocks ? ((int64_t)t.wk.n_blocks + U) * t.wk.M : 0;
     auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
     t.acc = 0;
     t.ml = up(rows * kD * 4);
     t.total = std::max<int64_t>(t.ml + up(rows * 8), 256);
     return t;
+}
+
+template <int CB, int RW, bool ROPE>
+int launch_tree_as(dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V, const uint16_t* q, const int32_t* seq_len, const TreeWork& wk,
+                   const TreeRope& rope, float* acc, float2* ml) {
+    const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, RW, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, kTreeSmem);
+    if (e != hipSuccess) return set_error(KVC_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
+    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(kTreeThreads), kTreeSmem, st, K, V, q, seq_len, wk, rope, acc, ml);
+    return check_launch("kvc_tree_attn");
+}
+
+template <bool ROPE>
+int launch_tree(const TreeLayout& t, dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V, const uint16_t* q, const int32_t* seq_len,
+                const TreeRope& rope, float* acc, float2* ml) {
+    if (t.cb == 2) return launch_tree_as<2, 8, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
+    if (t.rw == 8) return launch_tree_as<1, 8, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
+    if (t.rw == 4) return launch_tree_as<1, 4, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
+    return launch_tree_as<1, 2, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
 }
 
 int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok, int32_t max_seq_len) {
@@ -609,15 +840,6 @@ int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, in
         if (kct * 8 * k->r_host[u] * k->b_host[u] > INT32_MAX || vct * 8 * v->r_host[u] * v->b_host[u] > INT32_MAX)
             return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: a unit's stream exceeds 2 GiB");
     return KVC_OK;
-}
-
-template <int CB, bool ROPE>
-int launch_tree(dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V, const uint16_t* q, const int32_t* seq_len, const TreeWork& wk,
-                const TreeRope& rope, float* acc, float2* ml) {
-    const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, kTreeSmem);
-    if (e != hipSuccess) return set_error(KVC_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL((tree_partial_kernel<CB, ROPE>), grid, dim3(kTreeThreads), kTreeSmem, st, K, V, q, seq_len, wk, rope, acc, ml);
-    return check_launch("kvc_tree_attn");
 }
 
 }  // namespace
@@ -656,23 +878,25 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     float2* ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(ws) + t.ml);
     const hipStream_t st = (hipStream_t)stream;
     const DevSide K = dev_side(k), V = dev_side(v);
-    const int64_t blocks = (int64_t)k->n_units * t.wk.nrb * t.wk.n_chunks, fin = (int64_t)k->n_units * ((t.wk.M + kFinRows - 1) / kFinRows);
+    const int64_t blocks = (int64_t)t.wk.nrb * t.wk.n_blocks;
+    const int R = (int64_t)k->n_units * ((t.wk.M + 15) / 16) < device_cus() / 2 ? 4 : 16;
+    const int64_t fin = (int64_t)k->n_units * ((t.wk.M + R - 1) / R);
     if (blocks > INT32_MAX || fin > INT32_MAX) return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: too many units");
     if (blocks) {
         TreeRope rope;
         for (int j = 0; j < kD / 2; ++j)
             rope.freq[j] = rope_base != 0.f ? std::pow((double)rope_base, -2.0 * j / kD) / 6.283185307179586476925 : 0.0;
         const dim3 grid((unsigned)blocks);
-        int e;
-        if (rope_base != 0.f)
-            e = t.cb == 1 ? launch_tree<1, true>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml) : launch_tree<2, true>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
-        else
-            e = t.cb == 1 ? launch_tree<1, false>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml) : launch_tree<2, false>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
+        const int e = rope_base != 0.f ? launch_tree<true>(t, grid, st, K, V, q, seq_len, rope, acc, ml)
+                                       : launch_tree<false>(t, grid, st, K, V, q, seq_len, rope, acc, ml);
         if (e) return e;
     }
-    const hipError_t he = hipFuncSetAttribute((const void*)tree_finish_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kFinSmem);
-    if (he != hipSuccess) return set_error(KVC_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(he));
-    hipLaunchKernelGGL(tree_finish_kernel, dim3((unsigned)fin), dim3(kTreeThreads), kFinSmem, st, V, q, G, n_tok, xk, xk_unit_stride, xv,
-                       xv_unit_stride, mask, t.wk, acc, ml, out);
+    const dim3 grid((unsigned)fin), blk(kFinThreads);
+    if (R == 4)
+        hipLaunchKernelGGL(tree_finish_kernel<4>, grid, blk, kFinSmem, st, V, q, G, n_tok, xk, xk_unit_stride, xv, xv_unit_stride, mask, seq_len,
+                           t.wk, acc, ml, out);
+    else
+        hipLaunchKernelGGL(tree_finish_kernel<16>, grid, blk, kFinSmem, st, V, q, G, n_tok, xk, xk_unit_stride, xv, xv_unit_stride, mask, seq_len,
+                           t.wk, acc, ml, out);
     return check_launch("kvc_tree_attn");
 }

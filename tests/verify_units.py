@@ -63,12 +63,13 @@ class Units:
 def tree_reference(units, u, q, xk, xv, words, n, base):
     """fp64 rows of unit u and the bound on what the kernel's rows may differ by. q (N, G, d), xk and xv (N, d) fp16 arrays.
 
-    Roundings to fp16, each at most half a step, 2^-11 of the value: of every coordinate of a rotated cached key, which moves a
-    logit by 2^-11 |q * k_t| / sqrt(d) (2-norm of the elementwise product: the signs do not line up); of every weight, and below
-    2^-14 of the largest by 2^-25 of it; and of the result. The first two move the output by the root of the sum of squares of
-    w_t (v_t - o), of which eight are allowed, since half a step is the most that a rounding moves; the result's is added (half a step is 2^-25 below 2^-14). fp32
-    sums, angles (fp64, and rotations of at most 32 steps of 2^-23 in between) and the two-part projection are below 2^-18 of the
-    same terms."""
+    Roundings, each at most half a step: of every weight to fp16, 2^-11 of it, and below 2^-14 of the largest 2^-25 of that; of
+    every coordinate of a rotated cached key, whose rest after fp16 (2^-11 of it) is taken from its bf8 part (2^-3 off) times the
+    query cut to two fraction bits (2^-2 off), so that less than half of it is lost: a logit moves by 2^-12 |q * k_t| / sqrt(d)
+    (2-norm of the elementwise product: the signs do not line up). These move the output by the root of the sum of squares of
+    w_t (v_t - o), of which eight are allowed, since half a step is the most that a rounding moves; the result's own rounding is
+    added, 2^-11 of it and 2^-25 below 2^-14. fp32 sums, angles (fp64, and rotations of at most 32 steps of 2^-23 in between) and
+    the two-part projection are below 2^-18 of the same terms."""
     N, G, d = q.shape
     q = q.astype(np.float64).reshape(N * G, d)
     k, v = units.keys(u, n, base), units.values(u, n)
@@ -83,7 +84,7 @@ def tree_reference(units, u, q, xk, xv, words, n, base):
     p /= np.maximum(p.sum(axis=1, keepdims=True), 1e-300)
     vals = np.concatenate([v, xv])
     o = p @ vals
-    ds = np.concatenate([2.0 ** -11 * np.sqrt((q * q) @ (k * k).T) / math.sqrt(d), np.zeros((N * G, N))], axis=1)
+    ds = np.concatenate([2.0 ** -12 * np.sqrt((q * q) @ (k * k).T) / math.sqrt(d), np.zeros((N * G, N))], axis=1)
     w2 = (p * ds) ** 2 + (2.0 ** -11 * p) ** 2 + np.where(p > 0, (2.0 ** -25 * p.max(axis=1, keepdims=True)) ** 2, 0.0)
     var = w2 @ (vals * vals) - 2 * o * (w2 @ vals) + o * o * w2.sum(axis=1, keepdims=True)
     bound = 8 * np.sqrt(np.maximum(var, 0.0)) + 2.0 ** -11 * np.abs(o) + 2.0 ** -25 + 2.0 ** -18 * np.abs(vals).max(initial=0.0)
