@@ -9,6 +9,8 @@
 #define KVC_DECODE_PARTIALS_UNIT
 #include "kvc_decode.hip"
 
+#include <type_traits>
+
 #include "kvc_codes.h"
 
 namespace kvc {
@@ -38,6 +40,14 @@ __device__ __forceinline__ v8i lead_bits(const rc_h8 (&q)[4]) {
         r[2 * ks + 1] = (int)perm(d[3], d[2], 0x07050301u);
     }
     return r;
+}
+
+// Four values, times 2^11, as bf8.
+typedef short s2v __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ s2v bf8_pairs(const float (&x)[4]) {
+    s2v r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, x[0], x[1], 1.f / kTreeLoScale, false);
+    return __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, x[2], x[3], 1.f / kTreeLoScale, true);
 }
 
 struct TreeRope {
@@ -212,12 +222,14 @@ constexpr int kTreeSmem = kTreeBuf + 2 * kBufBytes;
 // A rotated key is fp16 and the rest of it bf8 at 2^11 times its size, met by the queries' leading bits (e5m2 is fp16's upper byte):
 // logits keep about 14 bits of the key for a quarter more matrix work, where fp16 alone would put an error of 2^-12 of
 // each coordinate into the weights.
-template <int CB, int RW, bool ROPE>
+template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
     constexpr int TW = kTreeWaves / RW, TB = TW > 4 ? 1 : 4 / TW;  // token parts, and key blocks of one
-    const int tid = threadIdx.x, wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // opaque: a lane's addresses are formed again for every piece, not kept across all of them
+    const int wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
     const int rw = wv % RW, tw = wv / RW;
     const int row0 = rb * wk.rows_pb + 16 * CB * rw;  // the wavefront's rows
     const int64_t prow = slot * wk.M;
@@ -270,13 +282,20 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const float qs = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f;  // step_K log2(e) / sqrt(128)
     const float lazy = kTreeLazy / qs;
     float m[CB];  // running maxima of the raw products
-    rc_f4 O[8][CB], L[CB];
+    rc_f4 O[NV][CB], L[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
         m[cb] = -INFINITY;
         L[cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < 8; ++n) O[n][cb] = L[cb];
+        for (int n = 0; n < NV; ++n) O[n][cb] = L[cb];
+    }
+    uint32_t toks[TB];  // the tokens of key rows 4 grp + v of the wavefront's blocks, v by byte, less 16 grp
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+        toks[t] = 0;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) toks[t] |= (uint32_t)tree_tok(bv, TB * tw + t, v) << (8 * v);
     }
     const _Float16 h1 = (_Float16)1.f;
     const rc_h8 ones = {h1, h1, h1, h1, h1, h1, h1, h1};
@@ -337,15 +356,31 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             a[i] = *reinterpret_cast<const rc_f4*>(mid + 16 * (2 * fh + i) + 4 * grp);
             b[i] = *reinterpret_cast<const rc_f4*>(mid + 16 * (2 * fh + i + 4) + 4 * grp);
         }
+        auto rebuild = [&](auto first) {  // matrix steps `first` and `first` + 1: eight operands in flight
+            constexpr int s0 = decltype(first)::value;
+            rc_h8 pa[2][2], pb[2][2];
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            if (s < 2 || nk > 1)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    a[i] = mfma_h(*reinterpret_cast<const rc_h8*>(pt + bt_block(i, s)), z[s], a[i]);
-                    b[i] = mfma_h(*reinterpret_cast<const rc_h8*>(pt + bt_block(i + 4, s)), z[s], b[i]);
+                    pa[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i, s0 + s));
+                    pb[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + 4, s0 + s));
                 }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    a[i] = mfma_h(pa[s][i], z[s0 + s], a[i]);
+                    b[i] = mfma_h(pb[s][i], z[s0 + s], b[i]);
+                }
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+        };
+        rebuild(std::integral_constant<int, 0>());
+        if (nk > 1) rebuild(std::integral_constant<int, 2>());
         rc_h8 hx, hy;
+        float m1 = -1.f;
+        asm volatile("" : "+s"(m1));  // opaque: x - hi stays one mixed-precision multiply-add that reads the half
         int lx[2] = {0, 0}, ly[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -356,13 +391,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 y[v] = ROPE ? fmaf(a[i][v], sn[i][v], b[i][v] * cs[i][v]) : b[i][v] * kRawScale;
                 hx[4 * i + v] = (_Float16)x[v];
                 hy[4 * i + v] = (_Float16)y[v];
-                x[v] = (x[v] - (float)hx[4 * i + v]) * kTreeLoScale;
-                y[v] = (y[v] - (float)hy[4 * i + v]) * kTreeLoScale;
+                x[v] = fmaf((float)hx[4 * i + v], m1, x[v]);
+                y[v] = fmaf((float)hy[4 * i + v], m1, y[v]);
             }
-            lx[i] = __builtin_amdgcn_cvt_pk_bf8_f32(x[0], x[1], lx[i], false);
-            lx[i] = __builtin_amdgcn_cvt_pk_bf8_f32(x[2], x[3], lx[i], true);
-            ly[i] = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], ly[i], false);
-            ly[i] = __builtin_amdgcn_cvt_pk_bf8_f32(y[2], y[3], ly[i], true);
+            lx[i] = __builtin_bit_cast(int, bf8_pairs(x));
+            ly[i] = __builtin_bit_cast(int, bf8_pairs(y));
         }
         uint8_t* dst = buf + (64 * grp + 16 * kb + col) * 16;
         *reinterpret_cast<rc_h8*>(dst + 4096 * fh) = hx;
@@ -395,13 +428,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             }
         }
         if ((tile + 1) * kTile > T) {  // the context's last tile
-            int bvo = bv;
-            asm volatile("" : "+s"(bvo));  // opaque: the tokens of the lane's rows are not kept across tiles
 #pragma unroll
             for (int t = 0; t < TB; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    if (tile * kTile + 16 * grp + tree_tok(bvo, tb0 + t, v) >= T)
+                    if (tile * kTile + 16 * grp + (int)(toks[t] >> (8 * v) & 255u) >= T)
 #pragma unroll
                         for (int cb = 0; cb < CB; ++cb) S[t][cb][v] = -INFINITY;
         }
@@ -427,7 +458,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                     m[cb] = t;
                     L[cb] *= al;
 #pragma unroll
-                    for (int n = 0; n < 8; ++n) O[n][cb] *= al;
+                    for (int n = 0; n < NV; ++n) O[n][cb] *= al;
                 }
             }
         }
@@ -435,7 +466,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         rc_h8 P[TB > 1 ? TB / 2 : 1][CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            const float off = m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs, kTreeShift);
+            const float off = TW > 1 && m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs, kTreeShift);
             if constexpr (TB == 1) P[0][cb] = rc_h8{};
 #pragma unroll
             for (int t = 0; t < TB; ++t)
@@ -455,12 +486,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[s][cb], L[cb]);
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
-                if (n < nvt) {
-                    const rc_h8 vf = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
+            for (int n = 0; n < NV; ++n) {  // N-tiles past the rank make rows that are not stored
+                const rc_h8 vf = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
 #pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf, P[s][cb], O[n][cb]);
-                }
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf, P[s][cb], O[n][cb]);
+            }
         }
     };
     __syncthreads();  // P_K^T
@@ -491,7 +521,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             if (row >= wk.M) continue;
             if (grp == 0) ml_out[prow + row] = float2{fmaf(m[cb], qs, -kTreeShift), L[cb][0]};
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
+            for (int n = 0; n < NV; ++n)
                 if (n < nvt) *reinterpret_cast<rc_f4*>(acc_out + (prow + row) * kD + 16 * n + 4 * grp) = O[n][cb];
         }
     } else {  // the token parts meet in LDS (the tiles' buffers)
@@ -510,7 +540,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         const float al = m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[0] - t) * qs);
         if (grp == 0) sums[16 * wv + col] = al * L[0][0];
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < NV; ++n)
             if (n < nvt) *reinterpret_cast<rc_f4*>(parts + (16 * wv + col) * kPitch + 16 * n + 4 * grp) = O[n][0] * al;
         __syncthreads();
         if (tw == 0 && grp == 0 && row0 + col < wk.M) {
@@ -575,7 +605,10 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2,
         if (t1 <= t0) continue;
         left -= t1 - t0;
         __syncthreads();  // LDS of the piece before, or of the count above, has been read
-        tree_piece<CB, RW, ROPE>(K, V, q, wk, rope, u, T, t0, t1, rb, (int64_t)b + u, acc_out, ml_out);
+        const int rv = uni(V.r[u]);
+        if (rv <= 64) tree_piece<CB, RW, ROPE, 4>(K, V, q, wk, rope, u, T, t0, t1, rb, (int64_t)b + u, acc_out, ml_out);
+        else if (rv <= 96) tree_piece<CB, RW, ROPE, 6>(K, V, q, wk, rope, u, T, t0, t1, rb, (int64_t)b + u, acc_out, ml_out);
+        else tree_piece<CB, RW, ROPE, 8>(K, V, q, wk, rope, u, T, t0, t1, rb, (int64_t)b + u, acc_out, ml_out);
     }
 }
 
