@@ -366,6 +366,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                     pa[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i, s0 + s));
                     pb[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + 4, s0 + s));
                 }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -373,8 +374,6 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                     a[i] = mfma_h(pa[s][i], z[s0 + s], a[i]);
                     b[i] = mfma_h(pb[s][i], z[s0 + s], b[i]);
                 }
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
         };
         rebuild(std::integral_constant<int, 0>());
         if (nk > 1) rebuild(std::integral_constant<int, 2>());
@@ -411,20 +410,39 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(qf[cb][ks]));
         const int tb0 = TB * tw;  // first key block of the wavefront's tokens
-        // ---- scores
+        // ---- scores: the low parts first. Operands are read kAhead products ahead; the order is fixed by hand (left to itself the
+        // compiler saves registers and waits for each read).
         rc_f4 S[TB][CB];
+        {
+            constexpr int kAhead = 4;
+            const uint8_t* kr = buf + (64 * grp + 16 * tb0 + col) * 16;
+            auto key = [&](int i) { return *reinterpret_cast<const rc_h8*>(kr + 4096 * (i / TB) + 256 * (i % TB)); };
+            v4i l0[TB], l1[TB];
+            rc_h8 kf[kAhead];
 #pragma unroll
-        for (int t = 0; t < TB; ++t) {
-            const uint8_t* kr = buf + (64 * grp + 16 * (tb0 + t) + col) * 16;
-            const v4i l0 = *reinterpret_cast<const v4i*>(kr + kBufLo), l1 = *reinterpret_cast<const v4i*>(kr + kBufLo + 4096);
-            const v8i lo = {l0[0], l0[1], l0[2], l0[3], l1[0], l1[1], l1[2], l1[3]};
+            for (int t = 0; t < TB; ++t) {
+                l0[t] = *reinterpret_cast<const v4i*>(kr + kBufLo + 256 * t);
+                l1[t] = *reinterpret_cast<const v4i*>(kr + kBufLo + 4096 + 256 * t);
+            }
+            v8i q8[CB];
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_lo(lo, lead_bits(qf[cb]), rc_f4{0.f, 0.f, 0.f, 0.f});
+            for (int cb = 0; cb < CB; ++cb) q8[cb] = lead_bits(qf[cb]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                const rc_h8 kf = *reinterpret_cast<const rc_h8*>(kr + 4096 * ks);
+            for (int t = 0; t < TB; ++t) {
+                const v8i lo = {l0[t][0], l0[t][1], l0[t][2], l0[t][3], l1[t][0], l1[t][1], l1[t][2], l1[t][3]};
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_h(kf, qf[cb][ks], S[t][cb]);
+                for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_lo(lo, q8[cb], rc_f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                for (int i = kAhead * t / TB; i < kAhead * (t + 1) / TB; ++i) kf[i] = key(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * TB; ++i) {
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) S[i % TB][cb] = mfma_h(kf[i % kAhead], qf[cb][i / TB], S[i % TB][cb]);
+                if (i + kAhead < 4 * TB) kf[i % kAhead] = key(i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if ((tile + 1) * kTile > T) {  // the context's last tile
@@ -437,6 +455,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                         for (int cb = 0; cb < CB; ++cb) S[t][cb][v] = -INFINITY;
         }
         // ---- online softmax
+        constexpr int NS = TB > 1 ? TB / 2 : 1;  // halves of a tile: one or two
+        const uint8_t* vr = buf + kBufV + (tb0 >> 1) * 1024 + lane * 16;
+        rc_h8 vf[NV];  // N-tiles past the rank make rows that are not stored
+#pragma unroll
+        for (int n = 0; n < NV; ++n) vf[n] = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
         float top[CB];
         bool raise = false;
 #pragma unroll
@@ -462,35 +485,50 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 }
             }
         }
-        // a row that has seen no token yet (a part of a short last tile) has every weight 0
-        rc_h8 P[TB > 1 ? TB / 2 : 1][CB];
+        // ---- weights and values: the second half's weights and operands while the first half multiplies
+        float off[CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)  // a row that has seen no token yet (a part of a short last tile) has every weight 0
+            off[cb] = TW > 1 && m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs, kTreeShift);
+        auto weight = [&](int s, int cb, int e) { return __builtin_amdgcn_exp2f(fmaf(S[TB > 1 ? 2 * s + (e >> 2) : 0][cb][e & 3], qs, off[cb])); };
+        rc_h8 P[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            const float off = TW > 1 && m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs, kTreeShift);
-            if constexpr (TB == 1) P[0][cb] = rc_h8{};
+            if constexpr (TB == 1) P[cb] = rc_h8{};
 #pragma unroll
-            for (int t = 0; t < TB; ++t)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const _Float16 p = (_Float16)__builtin_amdgcn_exp2f(fmaf(S[t][cb][v], qs, off));
-                    if constexpr (TB > 1) P[t >> 1][cb][4 * (t & 1) + v] = p;
-                    else P[0][cb][v] = p;
-                }
+            for (int e = 0; e < (TB > 1 ? 8 : 4); ++e) P[cb][e] = (_Float16)weight(0, cb, e);
             if constexpr (TB == 1)
-                if (tb0 & 1) P[0][cb] = __builtin_shufflevector(P[0][cb], P[0][cb], 4, 5, 6, 7, 0, 1, 2, 3);
+                if (tb0 & 1) P[cb] = __builtin_shufflevector(P[cb], P[cb], 4, 5, 6, 7, 0, 1, 2, 3);
         }
-        // ---- values
 #pragma unroll
-        for (int s = 0; s < (TB > 1 ? TB / 2 : 1); ++s) {
-            const uint8_t* vr = buf + kBufV + ((tb0 >> 1) + s) * 1024 + lane * 16;
+        for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[cb], L[cb]);
+        if constexpr (NS == 1) {
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[s][cb], L[cb]);
+            for (int n = 0; n < NV; ++n)
 #pragma unroll
-            for (int n = 0; n < NV; ++n) {  // N-tiles past the rank make rows that are not stored
-                const rc_h8 vf = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
+        } else {
+            float w1[CB][8];
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf, P[s][cb], O[n][cb]);
+            for (int n = 0; n < NV; ++n) {
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
+                vf[n] = *reinterpret_cast<const rc_h8*>(vr + 1024 + n * 2048);
+#pragma unroll
+                for (int i = 8 * CB * n / NV; i < 8 * CB * (n + 1) / NV; ++i) w1[i >> 3][i & 7] = weight(1, i >> 3, i & 7);
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) P[cb][e] = (_Float16)w1[cb][e];
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[cb], L[cb]);
+#pragma unroll
+            for (int n = 0; n < NV; ++n)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
         }
     };
     __syncthreads();  // P_K^T
