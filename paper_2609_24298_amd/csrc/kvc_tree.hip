@@ -151,16 +151,42 @@ __device__ __forceinline__ void pairs8(uint32_t w0, uint32_t w1, uint32_t w2, ui
 
 // The raw codes of a key field as an operand: the integer c in a half is the fp16 number c 2^-24, which the matrix cores
 // take exactly, so that neither an exponent nor the centring costs an instruction here (both are in the accumulator's
-// start and in the scale of the rotation).
-__device__ __forceinline__ void tree_k_frag(const uint32_t (&w)[kFieldWords], int b, uint32_t x, rc_h8 (&z)[2]) {
-    uint32_t c[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-    if (b & 8) {
-        const uint32_t sh = 8 * x;  // funnel shifts by its low five bits
-        pairs8(funnel(w[1], w[0], sh), funnel(w[2], w[1], sh), funnel(w[3], w[2], sh), funnel(w[4], w[3], sh), c);
+// start and in the scale of the rotation). Widths up to 4 have code of their own (two or four operations a dword), the
+// rest one path for all.
+template <int B>
+__device__ __forceinline__ void tree_k_codes(const uint32_t (&w)[kFieldWords], uint32_t x, uint32_t (&c)[8]) {
+    uint32_t n[8];
+    if constexpr (B == 4) {
+        plane_pairs<4, 0>(Fld{funnel(w[1], w[0], 4 * x), funnel(w[2], w[1], 4 * x), 0u, 0u}, false, c);
+    } else if constexpr (B >= 2) {
+        plane_pairs<2, B - 2>(Fld{funnel(w[4], w[3], 2 * x), 0u, 0u, 0u}, false, c);
+        if constexpr (B == 3) {
+            plane_pairs<1, 0>(Fld{funnel(w[6], w[5], x), 0u, 0u, 0u}, false, n);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) c[m] |= n[m];
+        }
+    } else {
+        plane_pairs<1, 0>(Fld{funnel(w[6], w[5], x), 0u, 0u, 0u}, false, c);
     }
-    if (b & 4) pairs4(funnel(w[1], w[0], 4 * x), funnel(w[2], w[1], 4 * x), c);
-    if (b & 2) pairs2(funnel(w[4], w[3], 2 * x), 2, c);
-    if (b & 1) pairs1(funnel(w[6], w[5], x), 1, c);
+}
+__device__ __forceinline__ void tree_k_frag(const uint32_t (&w)[kFieldWords], int b, uint32_t x, rc_h8 (&z)[2]) {
+    uint32_t c[8];
+    if (b == 1) tree_k_codes<1>(w, x, c);
+    else if (b == 2) tree_k_codes<2>(w, x, c);
+    else if (b == 3) tree_k_codes<3>(w, x, c);
+    else if (b == 4) tree_k_codes<4>(w, x, c);
+    else {
+#pragma unroll
+        for (int m = 0; m < 8; ++m) c[m] = 0u;
+        if (b & 8) {
+            const uint32_t sh = 8 * x;  // funnel shifts by its low five bits
+            pairs8(funnel(w[1], w[0], sh), funnel(w[2], w[1], sh), funnel(w[3], w[2], sh), funnel(w[4], w[3], sh), c);
+        } else {
+            pairs4(funnel(w[1], w[0], 4 * x), funnel(w[2], w[1], 4 * x), c);
+        }
+        if (b & 2) pairs2(funnel(w[4], w[3], 2 * x), 2, c);
+        if (b & 1) pairs1(funnel(w[6], w[5], x), 1, c);
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) z[h] = __builtin_bit_cast(rc_h8, v4u{c[4 * h], c[4 * h + 1], c[4 * h + 2], c[4 * h + 3]});
 }
@@ -188,19 +214,25 @@ __device__ __forceinline__ void tree_v_load(const __amdgpu_buffer_rsrc_t rs, int
 }
 // Centred value codes c - 2^(b-1) + 1/2 (exact: 512 + c under fp16's exponent of 512, then one addition). Not left raw like
 // the keys': over a long context the centre's share of the sum would swamp what remains of it.
-__device__ __forceinline__ void tree_v_frag(const uint32_t (&w)[4], int b, rc_h8 (&z)[2]) {
-    uint32_t c[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-    if (b & 8) pairs8(w[0], w[1], w[2], w[3], c);
-    if (b & 4) pairs4(w[0], w[1], c);
-    if (b & 2) pairs2(w[2], 2, c);
-    if (b & 1) pairs1(w[3], 1, c);
-    const _Float16 mid = (_Float16)(-512.f - ((float)(1 << (b - 1)) - 0.5f));
-    const rc_h2 mid2 = rc_h2{mid, mid};
-    uint32_t d[8];
+__device__ __forceinline__ void tree_v_frag(const uint32_t (&w)[4], int b, uint32_t e512, rc_h8 (&z)[2]) {
+    if (b == 1) k_pairs<1>({Fld{w[3], 0u, 0u, 0u}, Fld{}, Fld{}}, false, e512, z);
+    else if (b == 2) k_pairs<2>({Fld{w[2], 0u, 0u, 0u}, Fld{}, Fld{}}, false, e512, z);
+    else if (b == 3) k_pairs<3>({Fld{w[2], 0u, 0u, 0u}, Fld{w[3], 0u, 0u, 0u}, Fld{}}, false, e512, z);
+    else if (b == 4) k_pairs<4>({Fld{w[0], w[1], 0u, 0u}, Fld{}, Fld{}}, false, e512, z);
+    else {
+        uint32_t c[8];
+        if (b & 8) pairs8(w[0], w[1], w[2], w[3], c);
+        else pairs4(w[0], w[1], c);
+        if (b & 2) pairs2(w[2], 2, c);
+        if (b & 1) pairs1(w[3], 1, c);
+        const _Float16 mid = (_Float16)(-512.f - ((float)(1 << (b - 1)) - 0.5f));
+        const rc_h2 mid2 = rc_h2{mid, mid};
+        uint32_t d[8];
 #pragma unroll
-    for (int m = 0; m < 8; ++m) d[m] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(rc_h2, (c[m] << 1) | 0x60006000u) + mid2);
+        for (int m = 0; m < 8; ++m) d[m] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(rc_h2, (c[m] << 1) | e512) + mid2);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) z[h] = __builtin_bit_cast(rc_h8, v4u{d[4 * h], d[4 * h + 1], d[4 * h + 2], d[4 * h + 3]});
+        for (int h = 0; h < 2; ++h) z[h] = __builtin_bit_cast(rc_h8, v4u{d[4 * h], d[4 * h + 1], d[4 * h + 2], d[4 * h + 3]});
+    }
 }
 
 // ---------------------------------------------------------------- cached tokens
@@ -211,7 +243,8 @@ constexpr int kTreeThreads = 64 * kTreeWaves;
 constexpr int kTreeAdv = kBtBytes, kTreeMid = kTreeAdv + (kD / 2) * 8;  // and the centre's share of a rebuilt key
 constexpr int kTreeBuf = kTreeMid + kD * 4;
 constexpr int kBufLo = kTile * kD * 2, kBufV = kBufLo + kTile * kD, kBufBytes = kBufV + kTile * kD * 2;
-constexpr int kTreeSmem = kTreeBuf + 2 * kBufBytes;
+constexpr int kTreeLead = kTreeBuf + 2 * kBufBytes;  // the queries' leading bits: [wavefront][cb][2][lane]
+constexpr int tree_smem(int cb) { return kTreeLead + kTreeWaves * cb * 2048; }
 
 // Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, the
 // wavefronts make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
@@ -249,6 +282,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const int ktb = 8 * rk * bk, vtb = 8 * rv * bv;
     const auto krs = __builtin_amdgcn_make_buffer_rsrc((void*)kstream, (short)0, wk.k_cap_tiles * ktb, kRsrcWord3);
     const auto vrs = __builtin_amdgcn_make_buffer_rsrc((void*)vstream, (short)0, wk.v_cap_tiles * vtb, kRsrcWord3);
+    const uint32_t e512 = exp512();
     const int g16 = rk >> 4, rho = rk & 15, nk = (rk + 63) >> 6, nvt = (rv + 15) >> 4;
     const int fh = wv & 1, kb = wv >> 1;  // the feature half and token block that the wavefront rebuilds
     const int ktok = 16 * (col >> 2) + tree_tok(bv, kb, col & 3);
@@ -259,7 +293,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         xk[ks] = cg < g16 ? (uint32_t)(1024 * cg + 16 * ktok) : (cg == g16 && rho ? (uint32_t)(1024 * g16 + ktok * rho) : (uint32_t)(g16 ? 16 * ktok : rho * ktok));
     }
     const PlaneAt ka[2] = {tree_k_at(bk, rk, xk[0]), tree_k_at(bk, rk, xk[1])}, va = tree_v_at(bv, rv, wv, col, grp);
-    uint32_t kw[2][kFieldWords], vw[4];
+    uint32_t kw[2][kFieldWords] = {}, vw[4] = {};
     auto load = [&](int tile) {
         tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
         if (nk > 1) tree_k_load(krs, tile * ktb, bk, ka[1], kw[1]);
@@ -267,6 +301,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     };
     load(tile0);
     // queries: columns of the operand, features in the order of the rebuilt keys
+    uint8_t* lead = sm + kTreeLead + wv * CB * 2048 + lane * 16;
     rc_h8 qf[CB][4];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -278,6 +313,9 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             if (row >= wk.M) a = b = uint2{0u, 0u};
             qf[cb][ks] = __builtin_bit_cast(rc_h8, v4u{a.x, a.y, b.x, b.y});
         }
+        const v8i r = lead_bits(qf[cb]);  // for this wavefront alone
+        *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
+        *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
     }
     const float qs = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f;  // step_K log2(e) / sqrt(128)
     const float lazy = kTreeLazy / qs;
@@ -342,7 +380,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             }
         }
         if (wv < nvt) {
-            tree_v_frag(vw, bv, vz);
+            tree_v_frag(vw, bv, e512, vz);
             *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + lane * 16) = vz[0];
             *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + 1024 + lane * 16) = vz[1];
         }
@@ -404,11 +442,6 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     };
     // the wavefront's rows against its tokens of a tile
     auto attend = [&](int tile, const uint8_t* buf) {
-        // opaque, so that the leading bits are formed again for every tile and take no registers in between
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(qf[cb][ks]));
         const int tb0 = TB * tw;  // first key block of the wavefront's tokens
         // ---- scores: the low parts first. Operands are read kAhead products ahead; the order is fixed by hand (left to itself the
         // compiler saves registers and waits for each read).
@@ -426,7 +459,10 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             }
             v8i q8[CB];
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) q8[cb] = lead_bits(qf[cb]);
+            for (int cb = 0; cb < CB; ++cb) {
+                const v4i a = *reinterpret_cast<const v4i*>(lead + cb * 2048), b = *reinterpret_cast<const v4i*>(lead + cb * 2048 + 1024);
+                q8[cb] = v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < TB; ++t) {
@@ -880,9 +916,9 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
 template <int CB, int RW, bool ROPE>
 int launch_tree_as(dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V, const uint16_t* q, const int32_t* seq_len, const TreeWork& wk,
                    const TreeRope& rope, float* acc, float2* ml) {
-    const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, RW, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, kTreeSmem);
+    const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, RW, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, tree_smem(CB));
     if (e != hipSuccess) return set_error(KVC_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(kTreeThreads), kTreeSmem, st, K, V, q, seq_len, wk, rope, acc, ml);
+    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(kTreeThreads), tree_smem(CB), st, K, V, q, seq_len, wk, rope, acc, ml);
     return check_launch("kvc_tree_attn");
 }
 
