@@ -18,7 +18,9 @@ namespace {
 
 constexpr float kTreeShift = 10.f;  // softmax weights are 2^(s - m + 10): fp16 keeps 11 bits of them down to 2^-24 of the largest
 constexpr float kTreeLazy = 5.f;    // the running maximum is raised when a tile beats it by more: weights stay below 2^15
-constexpr int kTreeResync = 32;     // tiles between exact sines and cosines (in between they advance by a rotation)
+// Tiles between exact sines and cosines (in between they advance by a rotation of 64 positions, 2^-23 off each time). The
+// exact ones are the hardware's, of the angle in turns reduced in fp64: at most 2^-22.9 off over a whole turn (measured).
+constexpr int kTreeResync = 32;
 
 constexpr float kRawScale = 16777216.f;  // 2^24: a raw code in an fp16 operand is this times too small
 constexpr float kTreeLoScale = 2048.f;  // of the low part of a key
@@ -71,9 +73,10 @@ __device__ __forceinline__ int unit_tokens(const int32_t* __restrict__ seq_len, 
 __device__ __forceinline__ int unit_tiles(const int32_t* __restrict__ seq_len, int u, int max_seq) {
     return (unit_tokens(seq_len, u, max_seq) + kTile - 1) / kTile;
 }
-__device__ __forceinline__ int64_t run_tiles(int64_t total, int n_blocks) { return (total + n_blocks - 1) / n_blocks; }
+// (32 bits: the host refuses more tiles)
+__device__ __forceinline__ uint32_t run_tiles(uint32_t total, int n_blocks) { return (total + (uint32_t)n_blocks - 1u) / (uint32_t)n_blocks; }
 
-__device__ __forceinline__ int64_t wave_total(int64_t v) {
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) {
     for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
     return v;
 }
@@ -270,13 +273,6 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     uint8_t* sm = kvc_dsm;
     float2* adv = reinterpret_cast<float2*>(sm + kTreeAdv);
     float* mid = reinterpret_cast<float*>(sm + kTreeMid);
-    stage_basis_t<KVC_SIDE_K>(sm, K.basis + K.basis_off[u], rk, tid, kTreeThreads);
-    if (ROPE && tid < kD / 2) {
-        const double t = (double)kTile * rope.freq[tid];
-        float s, c;
-        sincospif(2.f * (float)(t - rint(t)), &s, &c);
-        adv[tid] = float2{c, s};
-    }
     const uint8_t* kstream = uni(K.codes + K.code_off[u]);
     const uint8_t* vstream = uni(V.codes + V.code_off[u]);
     const int ktb = 8 * rk * bk, vtb = 8 * rv * bv;
@@ -351,9 +347,9 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const double t = pos * rope.freq[p0 + 16 * i + v];
-                        sincospif(2.f * (float)(t - rint(t)), &sn[i][v], &cs[i][v]);
-                        cs[i][v] *= kRawScale;
-                        sn[i][v] *= kRawScale;
+                        const float f = (float)(t - rint(t));
+                        cs[i][v] = kRawScale * __builtin_amdgcn_cosf(f);
+                        sn[i][v] = kRawScale * __builtin_amdgcn_sinf(f);
                     }
             } else {
 #pragma unroll
@@ -567,6 +563,12 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
         }
     };
+    stage_basis_t<KVC_SIDE_K>(sm, K.basis + K.basis_off[u], rk, tid, kTreeThreads);
+    if (ROPE && tid < kD / 2) {
+        const double t = (double)kTile * rope.freq[tid];
+        const float f = (float)(t - rint(t));
+        adv[tid] = float2{__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f)};
+    }
     __syncthreads();  // P_K^T
     {   // the centre's share of a key, -(2^(b-1) - 1/2) sum_i P_i: features 16 wv + 4 grp + v, in every column
         const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
@@ -642,30 +644,29 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2,
     const int rb = blockIdx.x % wk.nrb, b = blockIdx.x / wk.nrb;
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6);
     // the block's run of tiles and where it begins: a thread counts the tiles of some consecutive units
-    int64_t* waves = reinterpret_cast<int64_t*>(kvc_dsm);  // [8] tiles of each wavefront's units, then the first unit and tile
+    uint32_t* waves = reinterpret_cast<uint32_t*>(kvc_dsm);  // [8] tiles of each wavefront's units, then the first unit and tile
     const int cu = (wk.U + kTreeThreads - 1) / kTreeThreads, u_lo = min(wk.U, tid * cu), u_hi = min(wk.U, u_lo + cu);
-    int64_t mine = 0;
+    uint32_t mine = 0;
     for (int i = u_lo; i < u_hi; ++i) mine += unit_tiles(seq_len, i, wk.max_seq);
-    int64_t upto = mine;  // within the wavefront
+    uint32_t upto = mine;  // within the wavefront
     for (int o = 1; o < 64; o <<= 1) {
-        const int64_t v = __shfl_up(upto, o);
+        const uint32_t v = __shfl_up(upto, o);
         if (lane >= o) upto += v;
     }
     if (lane == 63) waves[wv] = upto;
     __syncthreads();
-    int64_t total = 0, before = upto - mine;
+    uint32_t total = 0, before = upto - mine;
     for (int i = 0; i < kTreeWaves; ++i) {
         if (i < wv) before += waves[i];
         total += waves[i];
     }
-    const int64_t per = run_tiles(total, wk.n_blocks);
-    int64_t g = per * b;
-    const int64_t g1 = min(total, g + per);
+    const uint32_t per = run_tiles(total, wk.n_blocks);
+    const uint32_t g = min(total, per * b), g1 = min(total, g + per);
     if (g >= g1) return;
     if (g >= before && g < before + mine) {
         int u = u_lo;
-        int64_t at = before;
-        for (int n; at + (n = unit_tiles(seq_len, u, wk.max_seq)) <= g; ++u) at += n;
+        uint32_t at = before;
+        for (uint32_t n; at + (n = unit_tiles(seq_len, u, wk.max_seq)) <= g; ++u) at += n;
         waves[kTreeWaves] = u;
         waves[kTreeWaves + 1] = g - at;
     }
@@ -698,7 +699,7 @@ constexpr int kFinP = kFinX + KVC_TREE_MAX_TOKENS * kFinXPitch * 2;  // weights 
 constexpr int kFinPPitch = KVC_TREE_MAX_TOKENS + 8;
 constexpr int kFinRed = kFinP + kFinRows * kFinPPitch * 2;   // maxima and sums of the wavefronts [2][4][16], row maxima [16], 1 / sums [16]
 constexpr int kFinCount = kFinRed + (2 * 4 * 16 + 32) * 4;    // [8] tiles
-constexpr int kFinSmem = kFinCount + 8 * 8;
+constexpr int kFinSmem = kFinCount + 8 * 4;
 static_assert(kFinSmem <= 64 * 1024, "no attribute is set for it");
 
 // Block: R rows of one unit (columns of the products past R repeat the last row). z = sum_c acc_c 2^(m_c - M) over the unit's
@@ -722,15 +723,17 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
     float* red = reinterpret_cast<float*>(sm + kFinRed);
     float* big = red + 2 * 4 * 16;
     float* inv = big + 16;
-    int64_t* count = reinterpret_cast<int64_t*>(sm + kFinCount);  // tiles of all units and of those before u, by wavefront
+    uint32_t* count = reinterpret_cast<uint32_t*>(sm + kFinCount);  // tiles of all units and of those before u, by wavefront
     const int rv = uni(V.r[u]);
     const int row = min(row0 + min(col, R - 1), wk.M - 1);
     const uint64_t live = n_tok == 64 ? ~0ull : (1ull << n_tok) - 1ull;
     const uint64_t mine = mask[(int64_t)u * n_tok + row / G] & live;
+    // Everything that the block reads is requested as early as its address is known.
+    uint64_t named = lane < n_tok ? mask[(int64_t)u * n_tok + lane] & live : 0ull;
     int tiles = 0;
     if (wk.n_blocks > 0) {
         tiles = uni(unit_tiles(seq_len, u, wk.max_seq));
-        int64_t all = 0, before = 0;
+        uint32_t all = 0, before = 0;
         for (int i = tid; i < wk.U; i += kFinThreads) {
             const int n = unit_tiles(seq_len, i, wk.max_seq);
             all += n;
@@ -739,68 +742,54 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         all = wave_total(all);
         before = wave_total(before);
         if (lane == 0) { count[wv] = all; count[4 + wv] = before; }
-        if (tiles) stage_basis_t<KVC_SIDE_K>(sm, V.basis + V.basis_off[u], rv, tid, kFinThreads);
     }
     // drafted tokens that some row of the unit names
-    uint64_t named = lane < n_tok ? mask[(int64_t)u * n_tok + lane] & live : 0ull;
     for (int o = 1; o < 64; o <<= 1) named |= __shfl_xor(named, o);
-    for (int e = tid; e < KVC_TREE_MAX_TOKENS * (kD / 8); e += kFinThreads) {
-        const int t = e >> 4, c8 = e & 15;
-        uint4 v = {0u, 0u, 0u, 0u};
-        if ((named >> t) & 1) v = *reinterpret_cast<const uint4*>(xv + (int64_t)u * xv_stride + (int64_t)t * kD + 8 * c8);
-        *reinterpret_cast<uint4*>(xs + t * kFinXPitch + 8 * c8) = v;
+    constexpr int kXv = KVC_TREE_MAX_TOKENS * (kD / 8) / kFinThreads;
+    uint4 xr[kXv];
+#pragma unroll
+    for (int j = 0; j < kXv; ++j) {
+        const int e = tid + j * kFinThreads, t = e >> 4, c8 = e & 15;
+        xr[j] = uint4{0u, 0u, 0u, 0u};
+        if ((named >> t) & 1) xr[j] = *reinterpret_cast<const uint4*>(xv + (int64_t)u * xv_stride + (int64_t)t * kD + 8 * c8);
     }
-    // scores of the wavefront's sixteen drafted tokens (rows of the result) and the block's rows (columns)
-    float s[4];
+    uint4 kr[4], qr[4];  // the wavefront's sixteen drafted tokens, the block's rows
     {
         const int t = 16 * wv + col;
         const bool there = (named >> t) & 1;
-        const uint16_t* kr = xk + (int64_t)u * xk_stride + (int64_t)t * kD + 8 * grp;
-        const uint16_t* qr = q + ((int64_t)u * wk.M + row) * kD + 8 * grp;
-        rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f};
+        const uint16_t* kp = xk + (int64_t)u * xk_stride + (int64_t)t * kD + 8 * grp;
+        const uint16_t* qp = q + ((int64_t)u * wk.M + row) * kD + 8 * grp;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
-            uint4 a = {0u, 0u, 0u, 0u};
-            if (there) a = *reinterpret_cast<const uint4*>(kr + 32 * ks);
-            c = mfma_h(__builtin_bit_cast(rc_h8, a), *reinterpret_cast<const rc_h8*>(qr + 32 * ks), c);
+            kr[ks] = uint4{0u, 0u, 0u, 0u};
+            if (there) kr[ks] = *reinterpret_cast<const uint4*>(kp + 32 * ks);
+            qr[ks] = *reinterpret_cast<const uint4*>(qp + 32 * ks);
         }
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            s[v] = (mine >> (16 * wv + 4 * grp + v)) & 1 ? c[v] * (1.4426950408889634f * 0.08838834764831845f) : -INFINITY;
     }
-    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (grp == 0) red[wv * 16 + col] = top;
     __syncthreads();
-    // the threads of row mr: maxima and sums over the pieces, whose slots follow one another
+    // the threads of row mr merge its pieces, whose slots follow one another: maxima, sums, eight coordinates each
     const int mr = tid / (16 * CG), mi = tid % (16 * CG), mc = mi & 15, cg = mi >> 4;
     const int mrow = min(row0 + mr, wk.M - 1);
-    int64_t slot0 = 0;
-    int n_pieces = 0;
+    float Mp = -INFINITY, l = 0.f;
+    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (tiles) {
-        const int64_t before = (count[4] + count[5]) + (count[6] + count[7]);
-        const int64_t per = run_tiles((count[0] + count[1]) + (count[2] + count[3]), wk.n_blocks);
-        const int64_t b0 = before / per;
-        slot0 = b0 + u;
-        n_pieces = (int)((before + tiles - 1) / per - b0) + 1;
-    }
-    const float2* mlr = ml + slot0 * wk.M + mrow;
-    float M = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
-    for (int c = mi; c < n_pieces; c += 16 * CG) M = fmaxf(M, mlr[(int64_t)c * wk.M].x);
-#pragma unroll
-    for (int o = 1; o < 16 * CG; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-    const float Mf = M == -INFINITY ? 0.f : M;
-    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
-    {
+        const uint32_t before = (count[4] + count[5]) + (count[6] + count[7]);
+        const uint32_t per = run_tiles((count[0] + count[1]) + (count[2] + count[3]), wk.n_blocks);
+        const uint32_t b0 = before / per;
+        const int64_t slot0 = (int64_t)b0 + u;
+        const int n_pieces = (int)((before + (uint32_t)tiles - 1u) / per - b0) + 1;
+        const float2* mlr = ml + slot0 * wk.M + mrow;
         const bool have = 8 * mc < ((rv + 15) & ~15);
         const float* ar = acc + (slot0 * wk.M + mrow) * kD + (have ? 8 * mc : 0);
         const int64_t stride = (int64_t)wk.M * kD;
+        for (int c = mi; c < n_pieces; c += 16 * CG) Mp = fmaxf(Mp, mlr[(int64_t)c * wk.M].x);
+#pragma unroll
+        for (int o = 1; o < 16 * CG; o <<= 1) Mp = fmaxf(Mp, __shfl_xor(Mp, o));
 #pragma unroll 4
         for (int c = cg; c < n_pieces; c += CG) {
             const float2 v = mlr[(int64_t)c * wk.M];
             const float4 a = *reinterpret_cast<const float4*>(ar + c * stride), b = *reinterpret_cast<const float4*>(ar + c * stride + 4);
-            const float w = __builtin_amdgcn_exp2f(v.x - Mf);
+            const float w = __builtin_amdgcn_exp2f(v.x - Mp);
             l = fmaf(w, v.y, l);
             z[0] = fmaf(w, a.x, z[0]); z[1] = fmaf(w, a.y, z[1]); z[2] = fmaf(w, a.z, z[2]); z[3] = fmaf(w, a.w, z[3]);
             z[4] = fmaf(w, b.x, z[4]); z[5] = fmaf(w, b.y, z[5]); z[6] = fmaf(w, b.z, z[6]); z[7] = fmaf(w, b.w, z[7]);
@@ -813,6 +802,36 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
+        stage_basis_t<KVC_SIDE_K>(sm, V.basis + V.basis_off[u], rv, tid, kFinThreads);
+    }
+#pragma unroll
+    for (int j = 0; j < kXv; ++j) {
+        const int e = tid + j * kFinThreads;
+        *reinterpret_cast<uint4*>(xs + (e >> 4) * kFinXPitch + 8 * (e & 15)) = xr[j];
+    }
+    // scores of the drafted tokens (rows of the result) and the block's rows (columns)
+    float s[4];
+    {
+        rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) c = mfma_h(__builtin_bit_cast(rc_h8, kr[ks]), __builtin_bit_cast(rc_h8, qr[ks]), c);
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            s[v] = (mine >> (16 * wv + 4 * grp + v)) & 1 ? c[v] * (1.4426950408889634f * 0.08838834764831845f) : -INFINITY;
+    }
+    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    if (grp == 0) red[wv * 16 + col] = top;
+    __syncthreads();
+    float M = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
+    M = fmaxf(M, Mp);
+    const float Mf = M == -INFINITY ? 0.f : M;
+    {
+        const float w = __builtin_amdgcn_exp2f(Mp - Mf);
+        l *= w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] *= w;
     }
     if (mi == 0) big[mr] = Mf;
     __syncthreads();
@@ -943,6 +962,8 @@ int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, in
     if (max_seq_len > k->capacity || max_seq_len > v->capacity)
         return set_error(KVC_ENOSPACE, "kvc_tree_attn: max_seq_len exceeds capacity");
     const int64_t kct = ((int64_t)k->capacity + kTile - 1) / kTile, vct = ((int64_t)v->capacity + kTile - 1) / kTile;
+    if ((int64_t)k->n_units * (((int64_t)max_seq_len + kTile - 1) / kTile) > INT32_MAX / 2)
+        return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: more than 2^30 tiles of 64 tokens");
     for (int u = 0; u < k->n_units; ++u)  // byte offsets inside a stream are 32 bits
         if (kct * 8 * k->r_host[u] * k->b_host[u] > INT32_MAX || vct * 8 * v->r_host[u] * v->b_host[u] > INT32_MAX)
             return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: a unit's stream exceeds 2 GiB");
