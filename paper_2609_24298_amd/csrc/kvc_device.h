@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 
 #include "kvc.h"
@@ -121,6 +122,17 @@ inline int device_cus() {
         ncu = 256;
     }
     return ncu;
+}
+
+// Turns per position of the rotary pairs, base^(-2j/128) / 2 pi, j < 64: a product of two of sixteen powers each, so that a
+// call does not wait for 64 of them (two roundings of 2^-53).
+inline void rope_frequencies(float base, double* freq) {
+    double lo[8], hi[8];
+    for (int i = 0; i < 8; ++i) {
+        lo[i] = std::pow((double)base, -i / 64.0);
+        hi[i] = std::pow((double)base, -i / 8.0) / 6.283185307179586476925;
+    }
+    for (int j = 0; j < KVC_HEAD_DIM / 2; ++j) freq[j] = hi[j >> 3] * lo[j & 7];
 }
 
 inline int check_launch(const char* what) {

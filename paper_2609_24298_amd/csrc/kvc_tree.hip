@@ -1018,8 +1018,8 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     if (blocks > INT32_MAX || fin > INT32_MAX) return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: too many units");
     if (blocks) {
         TreeRope rope;
-        for (int j = 0; j < kD / 2; ++j)
-            rope.freq[j] = rope_base != 0.f ? std::pow((double)rope_base, -2.0 * j / kD) / 6.283185307179586476925 : 0.0;
+        for (int j = 0; j < kD / 2; ++j) rope.freq[j] = 0.0;
+        if (rope_base != 0.f) rope_frequencies(rope_base, rope.freq);
         const dim3 grid((unsigned)blocks);
         const int e = rope_base != 0.f ? launch_tree<true>(t, grid, st, K, V, q, seq_len, rope, acc, ml)
                                        : launch_tree<false>(t, grid, st, K, V, q, seq_len, rope, acc, ml);

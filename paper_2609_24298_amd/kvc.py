@@ -374,8 +374,27 @@ def kvc_reconstruct(side: Side, t0: int, n_tok: int, out, stream=None):
 F16, BF16, F32 = 0, 1, 2  # KVC_F16, KVC_BF16, KVC_F32 of include/kvc.h
 
 
-def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+def _is(t, dtype, n: int, dev: int) -> bool:
+    """A contiguous tensor of n elements of a type on device dev (checks of short calls: attribute reads are what they cost)."""
+    return t.dtype is dtype and t.numel() == n and t.is_contiguous() and t.get_device() == dev
+
+
+def _rows(x, dtype, shape, dev: int) -> int:
+    """Checks x (units, rows, d), rows of a unit contiguous; returns the elements between units."""
+    U, N, d = x.shape
+    su, sn, sd = x.stride()
+    assert x.dtype is dtype and U == shape[0] and N >= shape[1] and d == HEAD_DIM and x.get_device() == dev
+    assert sd == 1 and (sn == HEAD_DIM or N <= 1)
+    return su if U > 1 else N * HEAD_DIM
+
+
+def _here(dev: int, stream) -> int:
+    """The stream of a call on device dev, which has to be the current one."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    assert torch.cuda.current_device() == dev, "the tensors are not on the current device"
+    return stream.cuda_stream
 
 
 def kvc_norm_rope(q, k, v, pos, wq, wk, eps: float, rope_base: float, G: int, q_out, k_out, k_rot, v_out, stream=None):
@@ -385,29 +404,33 @@ def kvc_norm_rope(q, k, v, pos, wq, wk, eps: float, rope_base: float, G: int, q_
     q_out (n_seq * kv_heads, n_tok, G, d), k_out (not rotated), k_rot (rotated) and v_out (n_seq * kv_heads, n_tok, d).
     An input may be None with its outputs, and either key output."""
     import torch
-    x0 = next(t for t in (q, k, v) if t is not None)
-    n_seq, n_tok = x0.shape[0], x0.shape[1]
-    kv_heads = q.shape[2] // (G * HEAD_DIM) if q is not None else x0.shape[2] // HEAD_DIM
+    x0 = q if q is not None else k if k is not None else v
+    n_seq, n_tok, width = x0.shape
+    dt, dev = x0.dtype, x0.get_device()
+    kv_heads = width // (HEAD_DIM * G) if q is not None else width // HEAD_DIM
+    strides = []
     for x, heads in ((q, kv_heads * G), (k, kv_heads), (v, kv_heads)):
-        if x is not None:
-            assert x.dim() == 3 and x.shape == (n_seq, n_tok, heads * HEAD_DIM) and x.dtype == x0.dtype and x.device == x0.device
-            # a dimension of one element has no stride; otherwise one stride between tokens
-            assert x.numel() == 0 or (x.stride(2) == 1 and (n_seq == 1 or n_tok == 1 or x.stride(0) == n_tok * x.stride(1)))
-    for o, n in ((q_out, G), (k_out, 1), (k_rot, 1), (v_out, 1)):
-        if o is not None:
-            assert o.dtype == torch.float16 and o.is_contiguous() and o.device == x0.device
-            assert o.numel() == n_seq * kv_heads * n_tok * n * HEAD_DIM
-    for w in (wq, wk):
-        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == HEAD_DIM and w.device == x0.device)
-    assert pos is None or (pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == n_seq * n_tok and pos.device == x0.device)
-    dt = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}[x0.dtype]
-
-    def stride(x):
-        return 0 if x is None else int(x.stride(1) if n_tok > 1 else (x.stride(0) if n_seq > 1 else x.shape[2]))
-
-    _check(lib().kvc_norm_rope(_ptr(q), stride(q), _ptr(k), stride(k), _ptr(v), stride(v), dt, int(n_seq), int(n_tok),
-                               int(kv_heads), int(G), _ptr(wq), _ptr(wk), float(eps), _ptr(pos), float(rope_base),
-                               _ptr(q_out), _ptr(k_out), _ptr(k_rot), _ptr(v_out), _stream_ptr(stream)))
+        if x is None:
+            strides.append(0)
+            continue
+        s0, s1, s2 = x.stride()
+        # one stride between tokens (a dimension of one element has none of its own)
+        assert x.shape == (n_seq, n_tok, heads * HEAD_DIM) and x.dtype is dt and x.get_device() == dev
+        assert s2 == 1 and (n_seq <= 1 or n_tok <= 1 or s0 == n_tok * s1)
+        strides.append(s1 if n_tok > 1 else s0 if n_seq > 1 else heads * HEAD_DIM)
+    n = n_seq * kv_heads * n_tok * HEAD_DIM
+    half, f32 = torch.float16, torch.float32
+    assert q_out is None or _is(q_out, half, n * G, dev)
+    assert k_out is None or _is(k_out, half, n, dev)
+    assert k_rot is None or _is(k_rot, half, n, dev)
+    assert v_out is None or _is(v_out, half, n, dev)
+    assert wq is None or _is(wq, f32, HEAD_DIM, dev)
+    assert wk is None or _is(wk, f32, HEAD_DIM, dev)
+    assert pos is None or _is(pos, torch.int32, n_seq * n_tok, dev)
+    code = F16 if dt is half else BF16 if dt is torch.bfloat16 else F32 if dt is f32 else -1
+    p = [None if t is None else t.data_ptr() for t in (q, k, v, wq, wk, pos, q_out, k_out, k_rot, v_out)]
+    _check(lib().kvc_norm_rope(p[0], strides[0], p[1], strides[1], p[2], strides[2], code, n_seq, n_tok, kv_heads, G, p[3], p[4],
+                               eps, p[5], rope_base, p[6], p[7], p[8], p[9], _here(dev, stream)))
 
 
 def kvc_tree_attn_workspace(k: Side, v: Side, G: int, n_tok: int, max_seq_len: int) -> int:
@@ -423,19 +446,16 @@ def kvc_tree_attn(k: Side, v: Side, q, G: int, xk, xv, mask, seq_len, max_seq_le
     (n_units, >= n_tok, d), contiguous within a unit; mask: int64 or uint64 (n_units, n_tok), bit m of word n: token n
     attends to drafted token m; seq_len: int32 (n_units,); rope_base 0: cached keys are not rotated; ws: uint8 workspace."""
     import torch
-    U, N = k.n_units, q.shape[1]
-    assert q.dim() == 4 and q.shape == (U, N, G, HEAD_DIM) and q.dtype == torch.float16 and q.is_contiguous()
-    assert out.shape == q.shape and out.dtype == torch.float16 and out.is_contiguous()
-    for x in (xk, xv):
-        assert x.dim() == 3 and x.dtype == torch.float16 and x.shape[0] == U and x.shape[1] >= N and x.shape[2] == HEAD_DIM
-        assert (N == 1 or x.stride(1) == HEAD_DIM) and x.stride(2) == 1 and x.device == q.device
-    assert mask.dtype in (torch.int64, torch.uint64) and mask.shape == (U, N) and mask.is_contiguous()
-    assert seq_len.dtype == torch.int32 and seq_len.numel() == U and seq_len.is_contiguous() and v.n_units == U
-    assert q.device == out.device == mask.device == seq_len.device == ws.device == k.codes.device
-    _check(lib().kvc_tree_attn(ctypes.byref(k.desc), ctypes.byref(v.desc), _ptr(q), int(G), int(N), _ptr(xk),
-                               int(xk.stride(0)) if U > 1 else N * HEAD_DIM, _ptr(xv),
-                               int(xv.stride(0)) if U > 1 else N * HEAD_DIM, _ptr(mask), _ptr(seq_len), int(max_seq_len),
-                               float(rope_base), _ptr(out), _ptr(ws), ws.numel(), _stream_ptr(stream)))
+    U, half, dev = k.n_units, torch.float16, q.get_device()
+    assert q.dim() == 4 and v.n_units == U and k.codes.get_device() == dev and ws.get_device() == dev
+    N = q.shape[1]
+    assert q.shape == (U, N, G, HEAD_DIM) and q.dtype is half and q.is_contiguous() and _is(out, half, U * N * G * HEAD_DIM, dev)
+    sk, sv = _rows(xk, half, (U, N), dev), _rows(xv, half, (U, N), dev)
+    assert _is(mask, torch.int64, U * N, dev) or _is(mask, torch.uint64, U * N, dev)
+    assert _is(seq_len, torch.int32, U, dev)
+    _check(lib().kvc_tree_attn(k.desc, v.desc, q.data_ptr(), G, N, xk.data_ptr(), sk, xv.data_ptr(), sv, mask.data_ptr(),
+                               seq_len.data_ptr(), max_seq_len, rope_base, out.data_ptr(), ws.data_ptr(), ws.numel(),
+                               _here(dev, stream)))
 
 
 def kvc_append_rows(k: Side, v: Side, xk, xv, t0, n, rows=None, stream=None):
@@ -443,20 +463,17 @@ def kvc_append_rows(k: Side, v: Side, xk, xv, t0, n, rows=None, stream=None):
     rows[u, 0 .. n[u]) (int32 (n_units, max_n); None: the first n[u] rows) go to positions t0[u] .. of its streams.
     t0, n: int32 (n_units,)."""
     import torch
-    U, n_rows = k.n_units, xk.shape[1]
-    for x in (xk, xv):
-        assert x.dim() == 3 and x.dtype == torch.float16 and x.shape == (U, n_rows, HEAD_DIM) and x.device == k.codes.device
-        assert (n_rows <= 1 or x.stride(1) == HEAD_DIM) and x.stride(2) == 1
-    for t in (t0, n):
-        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == U and t.device == xk.device
-    assert rows is None or (rows.dtype == torch.int32 and rows.is_contiguous() and rows.dim() == 2 and rows.shape[0] == U
-                            and rows.device == xk.device)
-    assert v.n_units == U and v.codes.device == xk.device
-    max_n = n_rows if rows is None else rows.shape[1]
-    _check(lib().kvc_append_rows(ctypes.byref(k.desc), ctypes.byref(v.desc), _ptr(xk),
-                                 int(xk.stride(0)) if U > 1 else n_rows * HEAD_DIM, _ptr(xv),
-                                 int(xv.stride(0)) if U > 1 else n_rows * HEAD_DIM, int(n_rows), _ptr(rows), _ptr(t0),
-                                 _ptr(n), int(max_n), _stream_ptr(stream)))
+    U, half, i32, dev = k.n_units, torch.float16, torch.int32, xk.get_device()
+    n_rows = xk.shape[1]
+    assert xv.shape[1] == n_rows and v.n_units == U and k.codes.get_device() == dev and v.codes.get_device() == dev
+    sk, sv = _rows(xk, half, (U, n_rows), dev), _rows(xv, half, (U, n_rows), dev)
+    assert _is(t0, i32, U, dev) and _is(n, i32, U, dev)
+    max_n = n_rows
+    if rows is not None:
+        max_n = rows.shape[1]
+        assert rows.dim() == 2 and _is(rows, i32, U * max_n, dev)
+    _check(lib().kvc_append_rows(k.desc, v.desc, xk.data_ptr(), sk, xv.data_ptr(), sv, n_rows,
+                                 None if rows is None else rows.data_ptr(), t0.data_ptr(), n.data_ptr(), max_n, _here(dev, stream)))
 
 
 def kvc_read_probe(buf, sink, stream=None):
