@@ -1,5 +1,5 @@
 // Device half of libkvc, compression side: HIP kernels for CDNA4 (gfx950) and
-// their C-ABI launchers (kvc_encode, kvc_encode_kv). Decode attention lives in
+// their C-ABI launchers (kvc_encode, kvc_encode_kv, kvc_append_rows). Decode attention lives in
 // kvc_decode.hip, reconstruction in kvc_recon.hip.
 //
 // Kernels
@@ -12,10 +12,15 @@
 //                       rows read coalesced, the same bounded decision (undecided
 //                       elements settled by their wavefront), and the new fields
 //                       written in place (whole words where a token owns them).
+//  append_rows_kernel, encode_few_rows_kernel, encode_rows_kernel
+//                       chosen tokens, a count and a position per unit from the
+//                       device: the two kernels above over a unit's own run, and
+//                       between them a wavefront per tile.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 #include <utility>
 
 #include "kvc_append.h"
@@ -259,9 +264,30 @@ __device__ __forceinline__ void pack_v_field(const uint32_t (&c)[4], const uint3
     }
 }
 
+// Where a wavefront reads the basis of a group from: LDS, staged once per block (rows >= r zero), or global memory.
+struct StagedBasis {
+    static constexpr bool kAlone = false;
+    const uint16_t* __restrict__ p;  // [128][kPRow]
+    __device__ __forceinline__ h8 frag(int row, int at) const { return *reinterpret_cast<const h8*>(p + row * kPRow + at); }
+    __device__ __forceinline__ const uint16_t* row(int c) const { return p + c * kPRow; }
+};
+struct GlobalBasis {
+    static constexpr bool kAlone = true;  // each row once: its norm is formed on the way, and the next group's rows are requested ahead
+    const uint16_t* __restrict__ p;  // [r][kD], at any element
+    int r;
+    __device__ __forceinline__ h8 frag(int row, int at) const {
+        const uint4 v = row < r ? load_basis8(p + (int64_t)row * kD + at) : uint4{0u, 0u, 0u, 0u};
+        return __builtin_bit_cast(h8, v);
+    }
+    __device__ __forceinline__ const uint16_t* row(int c) const { return p + (int64_t)c * kD; }
+};
+
+template <class Basis>
+using PnormOf = std::conditional_t<Basis::kAlone, float*, const float*>;
+
 // The tiles of one wavefront: tl = tl0, tl0 + kEncWaves, ... below tl_end (indices into the call's tiles).
-template <int side, int B, class Rows>
-__device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, const float* __restrict__ pnrm, float tol,
+template <int side, int B, class Basis, class Rows>
+__device__ __forceinline__ void encode_tiles(const Basis& P, PnormOf<Basis> pnrm, float tol,
                                              float* __restrict__ etok, uint8_t* __restrict__ sb, const uint16_t* __restrict__ Pg,
                                              uint8_t* __restrict__ stream, const Rows& x, int r, float step,
                                              int t0, int n_tok, int tile_first, int tl0, int tl_end, int lane) {
@@ -328,7 +354,12 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
                 const f4 e = *reinterpret_cast<const f4*>(etok + 16 * nt + 4 * grp);
                 thr[nt] = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
             }
-            thr[nt] = fmaf(-thr[nt], tol, half_amb);
+            if constexpr (!Basis::kAlone) thr[nt] = fmaf(-thr[nt], tol, half_amb);
+        }
+        h8 pn[Basis::kAlone ? 4 : 1];  // the next group's rows
+        if constexpr (Basis::kAlone) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) pn[ks] = P.frag(col, 32 * ks + 8 * grp);
         }
         uint32_t vg[3][4], cm[4];  // V: value groups being gathered; all-ones codes at the field positions that are encoded
         if constexpr (side == KVC_SIDE_V) {
@@ -349,9 +380,34 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
 #pragma unroll 1
         for (int mc = 0; mc < n_mc; ++mc) {
             h8 pf[4];
+            float limit[4];  // an element of quarter nt is undecided from there on
+            if constexpr (Basis::kAlone) {
+                float s2 = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-                pf[ks] = *reinterpret_cast<const h8*>(Pl + (16 * mc + col) * kPRow + 32 * ks + 8 * grp);
+                for (int ks = 0; ks < 4; ++ks) {
+                    pf[ks] = pn[ks];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const h2 v = {pf[ks][2 * e], pf[ks][2 * e + 1]};
+                        s2 = __builtin_amdgcn_fdot2(v, v, s2, false);
+                    }
+                    if (mc + 1 < n_mc) pn[ks] = P.frag(16 * (mc + 1) + col, 32 * ks + 8 * grp);
+                }
+                s2 += __shfl_xor(s2, 16);
+                s2 += __shfl_xor(s2, 32);
+                const float n = sqrtf(s2);
+                if (grp == 0) pnrm[16 * mc + col] = n;
+                float most = n;  // of the group's rows
+                for (int o = 1; o < 16; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+                wave_lds_sync();
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) limit[nt] = fmaf(-thr[nt], tol * most, half_amb);
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) pf[ks] = P.frag(16 * mc + col, 32 * ks + 8 * grp);
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) limit[nt] = thr[nt];
+            }
             f4 acc[4];
 #pragma unroll
             for (int nt = 0; nt < 4; ++nt) {
@@ -392,7 +448,7 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
                     dmax = fmaxf(dmax, fabsf(tp - m));
                     w = __builtin_amdgcn_cvt_pk_u8_f32(__builtin_amdgcn_fmed3f(m, 0.f, fmax_code), i, w);
                 }
-                any_amb |= dmax >= thr[nt];
+                any_amb |= dmax >= limit[nt];
                 cw[nt] = w;
             }
             // undecided elements (rare): flag them per lane, then the whole wavefront settles them one by one
@@ -403,7 +459,7 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float tp = fmaf(acc[nt][i], inv, fh_lo);
-                        if (fabsf(tp - __builtin_rintf(tp)) >= thr[nt]) ambm |= 1u << (4 * nt + i);
+                        if (fabsf(tp - __builtin_rintf(tp)) >= limit[nt]) ambm |= 1u << (4 * nt + i);
                     }
                 // a token long enough makes thr negative and flags even the coordinates past the rank
                 if (mc == g16) ambm &= encode_rank_mask(side, r - 16 * mc, col, grp);
@@ -446,7 +502,7 @@ __device__ __forceinline__ void encode_tiles(const uint16_t* __restrict__ Pl, co
                         } else {
                             xw = *reinterpret_cast<const uint32_t*>(xrow + 2 * lane);
                         }
-                        const uint32_t code = resolve_code_wave(Pl + c * kPRow, Pg + (int64_t)c * kD, xw, xrow, step, inv64, B,
+                        const uint32_t code = resolve_code_wave(P.row(c), Pg + (int64_t)c * kD, xw, xrow, step, inv64, B,
                                                                 pnrm[c], etok[row], lane);
 #pragma unroll
                         for (int n = 0; n < 4; ++n)
@@ -523,10 +579,10 @@ __device__ __forceinline__ void encode_block(const DevSide& s, int side, int u, 
     const int tl0 = blockIdx.x * tpb + wv, tl_end = min((int)(blockIdx.x + 1) * tpb, n_tiles);
     uint8_t* __restrict__ stream = s.codes + s.code_off[u];
     if (side == KVC_SIDE_K) {
-        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_K, B_>(Pl, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, x, r,
+        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_K, B_>(StagedBasis{Pl}, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, x, r,
                                                       step, t0, n_tok, tile_first, tl0, tl_end, lane)));
     } else {
-        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_V, B_>(Pl, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, x, r,
+        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_V, B_>(StagedBasis{Pl}, pnrm, tol, etoks + wv * kTile, stages + wv * kEncStage, Pg, stream, x, r,
                                                       step, t0, n_tok, tile_first, tl0, tl_end, lane)));
     }
 }
@@ -561,18 +617,61 @@ __device__ __forceinline__ int rows_range(const RowsArgs& a, int side, int u, in
     return (int)(hi - lo);
 }
 
-// Few tokens per unit: block (u, side), kAppMaxTok tokens at a time.
+// One or two tokens per unit: block (u, side). Bound by latency: 10.0 us a call at 64 units, 24.4 at
+// 2048 (2 bits per dimension).
 __global__ __launch_bounds__(kAppThreads) void append_rows_kernel(DevSide ks, DevSide vs, RowsArgs a) {
     const int u = blockIdx.x, side = blockIdx.y;
     const DevSide& s = side == KVC_SIDE_K ? ks : vs;
     const uint16_t* xu = a.x[side] + (int64_t)u * a.stride[side];
     int i0 = 0, t = 0;
     const int n = rows_range(a, side, u, &i0, &t);
-    for (int i = 0; i < n; i += kAppMaxTok) {
-        if (i) __syncthreads();  // the codes of the turn before have been read
-        if (a.rows) append_tokens(s, side, ChosenRows{xu, a.rows + (int64_t)u * a.max_n + i0 + i, a.n_rows - 1}, t + i, min(n - i, kAppMaxTok), u);
-        else append_tokens(s, side, EveryRow{xu + (int64_t)(i0 + i) * kD}, t + i, min(n - i, kAppMaxTok), u);
+    if (n == 0) return;
+    if (a.rows) append_tokens(s, side, ChosenRows{xu, a.rows + (int64_t)u * a.max_n + i0, a.n_rows - 1}, t, n, u);
+    else append_tokens(s, side, EveryRow{xu + (int64_t)i0 * kD}, t, n, u);
+}
+
+// A few tokens per unit: a wavefront takes one tile of one unit and side, and reads the basis from global memory, since it
+// needs every row once: no staging, no barrier, and four times the units in flight of a block that stages for one tile. The
+// error bound's row norms are formed as the rows pass, and the next 16 rows are requested before these are used: 58 -> 45 us
+// at 2048 units of 5 tokens. Bound by the latency of those loads at two wavefronts a SIMD (the tile's accumulators and
+// codes hold 214 registers); the bases are most of its bytes.
+template <class Rows>
+__device__ __forceinline__ void encode_tile_alone(const DevSide& s, int side, int u, const Rows& x, int t0, int n_tok, int tile_first, int tl,
+                                                  float* __restrict__ pnrm, float* __restrict__ etok, uint8_t* __restrict__ stage, int lane) {
+    const int r = s.r[u], b = s.b[u];
+    const float step = s.delta[u];
+    const uint16_t* __restrict__ Pg = s.basis + s.basis_off[u];
+    const GlobalBasis P{Pg, r};
+    const float tol = 33.f * 0x1p-23f * 1.01f / step;  // times the largest norm of a group's rows
+    uint8_t* __restrict__ stream = s.codes + s.code_off[u];
+    if (side == KVC_SIDE_K) {
+        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_K, B_>(P, pnrm, tol, etok, stage, Pg, stream, x, r, step, t0, n_tok, tile_first, tl, tl + 1, lane)));
+    } else {
+        KVC_SWITCH_B(b, (encode_tiles<KVC_SIDE_V, B_>(P, pnrm, tol, etok, stage, Pg, stream, x, r, step, t0, n_tok, tile_first, tl, tl + 1, lane)));
     }
+}
+
+__global__ __launch_bounds__(kEncMmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void encode_few_rows_kernel(DevSide ks, DevSide vs,
+                                                                                                                    RowsArgs a, int n_units,
+                                                                                                                    int most_tiles) {
+    __shared__ float pnrm[kEncWaves][kD], etok[kEncWaves][kTile];
+    __shared__ __align__(16) uint8_t stage[kEncWaves][kEncStage];
+    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, side = blockIdx.y;
+    const int64_t item = (int64_t)blockIdx.x * kEncWaves + wv;
+    const int u = __builtin_amdgcn_readfirstlane((int)(item / most_tiles)), tl = __builtin_amdgcn_readfirstlane((int)(item % most_tiles));
+    if (u >= n_units) return;
+    const DevSide& s = side == KVC_SIDE_K ? ks : vs;
+    const uint16_t* xu = a.x[side] + (int64_t)u * a.stride[side];
+    int i0 = 0, t = 0;
+    const int n = rows_range(a, side, u, &i0, &t);
+    if (n == 0) return;
+    const int tile_first = t / kTile, n_tiles = (t + n - 1) / kTile - tile_first + 1;
+    if (tl >= n_tiles) return;
+    if (a.rows)
+        encode_tile_alone(s, side, u, ChosenRows{xu, a.rows + (int64_t)u * a.max_n + i0, a.n_rows - 1}, t, n, tile_first, tl, pnrm[wv], etok[wv],
+                          stage[wv], lane);
+    else
+        encode_tile_alone(s, side, u, EveryRow{xu + (int64_t)i0 * kD}, t, n, tile_first, tl, pnrm[wv], etok[wv], stage[wv], lane);
 }
 
 // Runs of tokens: block (run of tiles, unit, side).
@@ -625,8 +724,20 @@ int encode_tpb(int64_t units, int n_tiles) {
     return tpb;
 }
 
-// Tokens per unit up to which kvc_append_rows takes the few-token kernel.
-constexpr int kRowsAppendMax = 16;
+// Which kernel kvc_append_rows launches, by max_n and the units (2 bits per dimension, gathered rows, per call):
+// * up to kRowsAppendMax tokens a thread per coordinate, since a matrix instruction would work for one or two of 16 columns:
+//   one token at 64 / 2048 units 10.0 / 24.4 us, a wavefront per tile 12.8 / 31.7, staged blocks 11.8 / 82.2. (At four
+//   tokens it loses at 64 and 256 units, 12.2 to 17 us against 11 to 14, the more the longer its loop over them.)
+// * up to kRowsFewMax tokens a wavefront per tile, if there are kRowsFewUnits staged blocks for each CU, so that staging
+//   would be repeated by every turn of the device: 5 tokens at 256 / 512 / 2048 units 12.9 / 17.3 / 45.0 us against
+//   14.0 / 25.2 / 83.9 staged; at 64 units, where a turn is all there is, 12.8 against 12.1. 64 tokens: 16.3 / 20.5 / 68.1
+//   against 16.2 / 30.1 / 106; 128 tokens, three tiles to share the staged rows: 21.0 / 34.7 / 101 against 18.1 / 34.4 / 114,
+//   and 511 at 512 units 80.8 against 71.1.
+// * staged blocks otherwise.
+constexpr int kRowsAppendMax = 2;
+constexpr int kRowsFewMax = 64;
+constexpr int64_t kRowsFewUnits = 2;
+static_assert(kRowsAppendMax <= kAppMaxTok, "append_rows_kernel takes a call's tokens in one turn");
 
 constexpr size_t kEncSmem = (size_t)kD * kPRow * 2 + kD * 4 + kEncWaves * (kTile * 4 + kEncStage);
 
@@ -709,6 +820,11 @@ extern "C" int kvc_append_rows(const kvc_stream_desc* k, const kvc_stream_desc* 
     const RowsArgs a = {{xk, xv}, {xk_unit_stride, xv_unit_stride}, n_rows, max_n, {k->capacity, v->capacity}, rows, t0, n};
     if (max_n <= kRowsAppendMax) {
         hipLaunchKernelGGL(append_rows_kernel, dim3(k->n_units, 2), dim3(kAppThreads), 0, (hipStream_t)stream, dev_side(k), dev_side(v), a);
+    } else if (max_n <= kRowsFewMax && 2ll * k->n_units >= kRowsFewUnits * device_cus()) {
+        const int most = (max_n + 2 * kTile - 2) / kTile;  // tiles of the longest run, wherever in a tile it begins
+        const int64_t blocks = ((int64_t)k->n_units * most + kEncWaves - 1) / kEncWaves;
+        hipLaunchKernelGGL(encode_few_rows_kernel, dim3((unsigned)blocks, 2), dim3(kEncMmaThreads), 0, (hipStream_t)stream, dev_side(k), dev_side(v),
+                           a, k->n_units, most);
     } else {
         const int n_tiles = (max_n + 2 * kTile - 2) / kTile;  // of the longest run, wherever in a tile it begins
         const int tpb = encode_tpb(2ll * k->n_units, n_tiles);

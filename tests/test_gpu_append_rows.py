@@ -61,6 +61,20 @@ def test_every_width(max_n):
     run(units, xk, xv, pick, t0, n)
 
 
+@pytest.mark.parametrize("max_n", [1, 3, 8, 17, 64, 66])
+@pytest.mark.parametrize("scale", [1.0, 900.0])
+def test_more_units_than_the_device_has_units_of_work(max_n, scale):
+    # enough units that the kernel with a wavefront per tile is chosen (up to 64 tokens) on 256 compute units, and some more
+    rows = [(RANKS[i % 10], 1 + i // 8 % 8, RANKS[(3 * i + i // 10) % 10], 1 + i % 8) for i in range(259)]
+    units, rng = Units(rows, 150, max_n), np.random.default_rng(max_n)
+    n_rows = max_n + 2
+    xk, xv = tokens(259, n_rows, 21, scale), tokens(259, n_rows, 22, scale)
+    pick = np.stack([rng.integers(0, n_rows, max_n) for _ in range(259)])
+    n = np.array([max_n if u % 4 == 0 else int(rng.integers(0, max_n + 1)) for u in range(259)])
+    t0 = np.array([int(rng.integers(-2, 150)) for _ in range(259)])
+    run(units, xk, xv, pick, t0, n)
+
+
 @pytest.mark.parametrize("max_n", [5, 70])
 def test_rows_repeated_and_all_of_them(max_n):
     units = Units([(84, 3, 64, 2), (128, 2, 126, 1), (18, 7, 30, 8)], 200, 5)
