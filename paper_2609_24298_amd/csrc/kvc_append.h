@@ -234,6 +234,7 @@ __device__ __forceinline__ void append_tokens(const DevSide& s, int side, const 
         }
     }
     __syncthreads();
+    if (i >= r) return;
     // Merge, per new token and plane. K: a token's 16 codes of a full coordinate group are 16
     // consecutive slots, i.e. whole 16-bit (p = 1) or 32-bit words that belong to this token alone:
     // the group's lanes OR their fields together and one lane per word stores it. The tail group's
@@ -242,7 +243,7 @@ __device__ __forceinline__ void append_tokens(const DevSide& s, int side, const 
     // One thread owns each coordinate, so the new tokens of a call are written in order.
     uint8_t* __restrict__ stream = s.codes + s.code_off[u];
     const int g16 = r >> 4, rho = r & 15;
-    for (int t = 0; t < (i < r ? n_tok : 0); ++t) {
+    for (int t = 0; t < n_tok; ++t) {
         const int tok = t0 + t, tile = tok / KVC_TILE_TOKENS, tt = tok % KVC_TILE_TOKENS;
         uint8_t* __restrict__ tbase = stream + (int64_t)tile * 8 * r * b;
         const uint32_t c = cs[t][i];
