@@ -224,6 +224,26 @@ class Cache:
         """Fused decode step: append (xk, xv) at t_new to every unit, then decode attention."""
         kvc.kvc_decode_step(self.K, self.V, xk, xv, t_new, q, self.w.group, seq_len, max_seq_len, out, ws, stream)
 
+    def verify_buffers(self, n_tok: int, max_seq_len: int, sides=None):
+        """Workspace and output for verify() of n_tok drafted tokens per unit, of all units or of the units of `sides`."""
+        import torch
+        K, V = sides or (self.K, self.V)
+        nbytes = kvc.kvc_tree_attn_workspace(K, V, self.w.group, n_tok, max_seq_len)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        out = torch.empty((K.n_units, n_tok, self.w.group, self.w.d), dtype=torch.float16, device=self.device)
+        return ws, out
+
+    def verify(self, q, xk, xv, mask, seq_len, max_seq_len: int, out, ws, rope_base: float = 0.0, sides=None, stream=None):
+        """Attention of a tree of drafted tokens over the cache and itself, of all units or of the units of `sides`
+        (layer_sides). q, xk, xv, mask, seq_len: as kvc.kvc_tree_attn (kvc.kvc_norm_rope lays out q, xk and xv)."""
+        K, V = sides or (self.K, self.V)
+        kvc.kvc_tree_attn(K, V, q, self.w.group, xk, xv, mask, seq_len, max_seq_len, rope_base, out, ws, stream)
+
+    def accept(self, xk, xv, t0, n, rows=None, sides=None, stream=None):
+        """Append the accepted drafted tokens, rows[u, :n[u]] of xk and xv (keys before their rotation), at t0[u]."""
+        K, V = sides or (self.K, self.V)
+        kvc.kvc_append_rows(K, V, xk, xv, t0, n, rows, stream)
+
     def layer_sides(self, layer: int):
         """Descriptors of one layer's units (u = (layer * batch + sequence) * kv_heads + head is
         layer-major, so they are one contiguous range) for per-layer calls."""
