@@ -23,6 +23,7 @@ constexpr float kTreeLazy = 5.f;    // the running maximum is raised when a tile
 constexpr int kTreeResync = 32;
 
 constexpr float kRawScale = 16777216.f;  // 2^24: a raw code in an fp16 operand is this times too small
+constexpr float kPlainScale = 0.0625f;   // of projected queries: one of the longest fp16 vector stays in range
 constexpr float kTreeLoScale = 2048.f;  // of the low part of a key
 constexpr int kTreeLoExp = 127 - 11;    // its scale as a matrix operand's exponent
 
@@ -249,7 +250,9 @@ constexpr int kTreeWaves = 8;
 constexpr int kTreeThreads = 64 * kTreeWaves;
 // LDS: P_K^T, the rotation of 64 positions, then two buffers of a tile's keys (fp16), their low parts (bf8) and values (fp16)
 constexpr int kTreeAdv = kBtBytes, kTreeMid = kTreeAdv + (kD / 2) * 8;  // and the centre's share of a rebuilt key
-constexpr int kTreeBuf = kTreeMid + kD * 4;
+constexpr int kTreePRow = kD + 8;  // plain keys: P_K at 0 instead, in rows of this many elements
+constexpr int kTreeBuf = kD * kTreePRow * 2;
+static_assert(kTreeMid + kD * 4 <= kTreeBuf);
 constexpr int kBufLo = kTile * kD * 2, kBufV = kBufLo + kTile * kD, kBufBytes = kBufV + kTile * kD * 2;
 constexpr int kTreeLead = kTreeBuf + 2 * kBufBytes;  // the queries' leading bits: [wavefront][cb][2][lane]
 constexpr int tree_smem(int cb) { return kTreeLead + kTreeWaves * cb * 2048; }
@@ -267,7 +270,7 @@ template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
-    constexpr int TW = kTreeWaves / RW, TB = TW > 4 ? 1 : 4 / TW;  // token parts, and key blocks of one
+    constexpr int TW = kTreeWaves / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // opaque: a lane's addresses are formed again for every piece, not kept across all of them
     const int wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
@@ -287,38 +290,117 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const int g16 = rk >> 4, rho = rk & 15, nk = (rk + 63) >> 6, nvt = (rv + 15) >> 4;
     const int fh = wv & 1, kb = wv >> 1;  // the feature half and token block that the wavefront rebuilds
     const int ktok = 16 * (col >> 2) + tree_tok(bv, kb, col & 3);
-    uint32_t xk[2];
+    constexpr int KU = ROPE ? 2 : 1;  // 64-coordinate parts of the keys' codes that a wavefront unpacks: all, or part fh
+    uint32_t xk[KU];
+    PlaneAt ka[KU];
+    uint32_t kw[KU][kFieldWords] = {}, vw[4] = {};
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-        const int cg = 4 * ks + grp;  // a group past the rank reads the first one (its columns of P_K^T are zero)
+    for (int ks = 0; ks < KU; ++ks) {
+        const int cg = 4 * (ROPE ? ks : fh) + grp;  // a group past the rank reads the first one (its columns of P_K^T are zero)
         xk[ks] = cg < g16 ? (uint32_t)(1024 * cg + 16 * ktok) : (cg == g16 && rho ? (uint32_t)(1024 * g16 + ktok * rho) : (uint32_t)(g16 ? 16 * ktok : rho * ktok));
+        ka[ks] = tree_k_at(bk, rk, xk[ks]);
     }
-    const PlaneAt ka[2] = {tree_k_at(bk, rk, xk[0]), tree_k_at(bk, rk, xk[1])}, va = tree_v_at(bv, rv, wv, col, grp);
-    uint32_t kw[2][kFieldWords] = {}, vw[4] = {};
+    const PlaneAt va = tree_v_at(bv, rv, wv, col, grp);
     auto load = [&](int tile) {
-        tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
-        if (nk > 1) tree_k_load(krs, tile * ktb, bk, ka[1], kw[1]);
+        if constexpr (ROPE) {
+            tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
+            if (nk > 1) tree_k_load(krs, tile * ktb, bk, ka[KU - 1], kw[KU - 1]);
+        } else if (fh < nk) {
+            tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
+        }
         if (wv < nvt) tree_v_load(vrs, tile * vtb, bv, va, vw);
     };
     load(tile0);
-    // queries: columns of the operand, features in the order of the rebuilt keys
+    // queries: columns of the operand. Rotated keys: features in the order of the rebuilt keys, and their leading bits.
+    // Plain keys: the projections onto the basis, in the order of the unpacked codes, as the sum of two fp16 (2^-22 of them)
+    constexpr int QW = ROPE ? 1 : 2;
     uint8_t* lead = sm + kTreeLead + wv * CB * 2048 + lane * 16;
-    rc_h8 qf[CB][4];
+    rc_h8 qf[QW][CB][4];
+    float base[CB];  // the centre's share of a row's raw products, -(2^(b-1) - 1/2) sum_i q_i
+    if constexpr (ROPE) {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        const int row = row0 + 16 * cb + col;
-        const uint16_t* qr = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD + 4 * grp;
+        for (int cb = 0; cb < CB; ++cb) {
+            const int row = row0 + 16 * cb + col;
+            const uint16_t* qr = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD + 4 * grp;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint2 a = *reinterpret_cast<const uint2*>(qr + 32 * ks), b = *reinterpret_cast<const uint2*>(qr + 32 * ks + 16);
-            if (row >= wk.M) a = b = uint2{0u, 0u};
-            qf[cb][ks] = __builtin_bit_cast(rc_h8, v4u{a.x, a.y, b.x, b.y});
+            for (int ks = 0; ks < 4; ++ks) {
+                uint2 a = *reinterpret_cast<const uint2*>(qr + 32 * ks), b = *reinterpret_cast<const uint2*>(qr + 32 * ks + 16);
+                if (row >= wk.M) a = b = uint2{0u, 0u};
+                qf[0][cb][ks] = __builtin_bit_cast(rc_h8, v4u{a.x, a.y, b.x, b.y});
+            }
+            const v8i r = lead_bits(qf[0][cb]);  // for this wavefront alone
+            *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
+            *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
+            base[cb] = 0.f;
         }
-        const v8i r = lead_bits(qf[cb]);  // for this wavefront alone
-        *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
-        *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
+    } else {
+        rc_h8 qr[CB][4];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const int row = row0 + 16 * cb + col;
+            const uint16_t* qp = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD + 8 * grp;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                uint4 a = *reinterpret_cast<const uint4*>(qp + 32 * ks);
+                if (row >= wk.M) a = uint4{0u, 0u, 0u, 0u};
+                qr[cb][ks] = __builtin_bit_cast(rc_h8, a);
+            }
+        }
+        // the basis, staged for all wavefronts (rows past the rank zero)
+        uint16_t* Pl = reinterpret_cast<uint16_t*>(sm);
+        const uint16_t* Pg = K.basis + K.basis_off[u];
+        uint4 pr[kD * kD / 8 / kTreeThreads];
+#pragma unroll
+        for (int j = 0; j < kD * kD / 8 / kTreeThreads; ++j) {
+            const int e = tid + j * kTreeThreads;
+            pr[j] = uint4{0u, 0u, 0u, 0u};
+            if (e < rk * (kD / 8)) pr[j] = load_basis8(Pg + 8 * e);
+        }
+#pragma unroll
+        for (int j = 0; j < kD * kD / 8 / kTreeThreads; ++j) {
+            const int e = tid + j * kTreeThreads;
+            *reinterpret_cast<uint4*>(Pl + (e >> 4) * kTreePRow + 8 * (e & 15)) = pr[j];
+        }
+        __syncthreads();
+        const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
+        const rc_h8 cc = {c, c, c, c, c, c, c, c};
+        rc_f4 sum[CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) sum[cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {  // coordinates 64 (ks / 2) + 16 grp + 4 (ks % 2) + v, and 8 further
+            rc_f4 d[2][CB];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = 64 * (ks >> 1) + 16 * (col >> 2) + 4 * (ks & 1) + (col & 3) + 8 * h;
+                rc_h8 p[4];
+#pragma unroll
+                for (int fs = 0; fs < 4; ++fs) p[fs] = *reinterpret_cast<const rc_h8*>(Pl + i * kTreePRow + 32 * fs + 8 * grp);
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    d[h][cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int fs = 0; fs < 4; ++fs) d[h][cb] = mfma_h(p[fs], qr[cb][fs], d[h][cb]);
+                }
+            }
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = d[e & 1][cb][e >> 1] * kPlainScale;
+                    const _Float16 hi = (_Float16)x;
+                    qf[0][cb][ks][e] = hi;
+                    qf[QW - 1][cb][ks][e] = (_Float16)(x - (float)hi);
+                }
+                sum[cb] = mfma_h(cc, qf[0][cb][ks], sum[cb]);
+                sum[cb] = mfma_h(cc, qf[QW - 1][cb][ks], sum[cb]);
+            }
+        }
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) base[cb] = sum[cb][0] * (1.f / kRawScale);
     }
-    const float qs = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f;  // step_K log2(e) / sqrt(128)
+    // step_K log2(e) / sqrt(128), and what scales a raw product
+    const float qs = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f * (ROPE ? 1.f : kRawScale / kPlainScale);
     const float lazy = kTreeLazy / qs;
     float m[CB];  // running maxima of the raw products
     rc_f4 O[NV][CB], L[CB];
@@ -369,16 +451,22 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             }
         }
         rc_h8 z[4], vz[2];
-        {
+        if constexpr (ROPE) {
             rc_h8 zz[2];
             tree_k_frag(kw[0], bk, xk[0], zz);
             z[0] = zz[0];
             z[1] = zz[1];
             if (nk > 1) {
-                tree_k_frag(kw[1], bk, xk[1], zz);
+                tree_k_frag(kw[KU - 1], bk, xk[KU - 1], zz);
                 z[2] = zz[0];
                 z[3] = zz[1];
             }
+        } else if (fh < nk) {
+            rc_h8 zz[2];
+            tree_k_frag(kw[0], bk, xk[0], zz);
+            uint8_t* dst = buf + 8192 * fh + (64 * grp + 16 * kb + col) * 16;
+            *reinterpret_cast<rc_h8*>(dst) = zz[0];
+            *reinterpret_cast<rc_h8*>(dst + 4096) = zz[1];
         }
         if (wv < nvt) {
             tree_v_frag(vw, bv, e512, vz);
@@ -386,6 +474,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + 1024 + lane * 16) = vz[1];
         }
         if (tile + 1 < tile1) load(tile + 1);
+        if constexpr (!ROPE) return;
         int po = bt_lane(col, grp) + bt_block(2 * fh, 0);
         asm volatile("" : "+v"(po));  // opaque: P_K^T is read again for every tile and takes no registers in between
         const uint8_t* pt = sm + po;
@@ -425,8 +514,8 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             float x[4], y[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                x[v] = ROPE ? fmaf(a[i][v], cs[i][v], -b[i][v] * sn[i][v]) : a[i][v] * kRawScale;
-                y[v] = ROPE ? fmaf(a[i][v], sn[i][v], b[i][v] * cs[i][v]) : b[i][v] * kRawScale;
+                x[v] = fmaf(a[i][v], cs[i][v], -b[i][v] * sn[i][v]);
+                y[v] = fmaf(a[i][v], sn[i][v], b[i][v] * cs[i][v]);
                 hx[4 * i + v] = (_Float16)x[v];
                 hy[4 * i + v] = (_Float16)y[v];
                 x[v] = fmaf((float)hx[4 * i + v], m1, x[v]);
@@ -447,7 +536,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         // ---- scores: the low parts first. Operands are read kAhead products ahead; the order is fixed by hand (left to itself the
         // compiler saves registers and waits for each read).
         rc_f4 S[TB][CB];
-        {
+        if constexpr (ROPE) {
             constexpr int kAhead = 4;
             const uint8_t* kr = buf + (64 * grp + 16 * tb0 + col) * 16;
             auto key = [&](int i) { return *reinterpret_cast<const rc_h8*>(kr + 4096 * (i / TB) + 256 * (i % TB)); };
@@ -477,10 +566,31 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int i = 0; i < 4 * TB; ++i) {
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) S[i % TB][cb] = mfma_h(kf[i % kAhead], qf[cb][i / TB], S[i % TB][cb]);
+                for (int cb = 0; cb < CB; ++cb) S[i % TB][cb] = mfma_h(kf[i % kAhead], qf[0][cb][i / TB], S[i % TB][cb]);
                 if (i + kAhead < 4 * TB) kf[i % kAhead] = key(i + kAhead);
                 __builtin_amdgcn_sched_barrier(0);
             }
+        } else {
+            const uint8_t* kr = buf + (64 * grp + 16 * tb0 + col) * 16;
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) S[t][cb] = rc_f4{base[cb], base[cb], base[cb], base[cb]};
+            auto part = [&](auto first) {  // matrix steps `first` and `first` + 1
+                constexpr int s0 = decltype(first)::value;
+                rc_h8 kf[2 * TB];
+#pragma unroll
+                for (int i = 0; i < 2 * TB; ++i) kf[i] = *reinterpret_cast<const rc_h8*>(kr + 4096 * (s0 + i / TB) + 256 * (i % TB));
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 2 * TB; ++i)
+#pragma unroll
+                    for (int w = 0; w < QW; ++w)
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb) S[i % TB][cb] = mfma_h(kf[i], qf[w][cb][s0 + i / TB], S[i % TB][cb]);
+            };
+            part(std::integral_constant<int, 0>());
+            if (nk > 1) part(std::integral_constant<int, 2>());
         }
         if ((tile + 1) * kTile > T) {  // the context's last tile
 #pragma unroll
@@ -568,8 +678,9 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
         }
     };
+    if constexpr (ROPE) {
     stage_basis_t<KVC_SIDE_K>(sm, K.basis + K.basis_off[u], rk, tid, kTreeThreads);
-    if (ROPE && tid < kD / 2) {
+    if (tid < kD / 2) {
         const double t = (double)kTile * rope.freq[tid];
         const float f = (float)(t - rint(t));
         adv[tid] = float2{__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f)};
@@ -584,6 +695,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         if (col == 0) *reinterpret_cast<rc_f4*>(mid + 16 * wv + 4 * grp) = a * (1.f / kRawScale);
     }
     __syncthreads();
+    }
     const bool late = wv >= kTreeWaves / 2;
 #pragma unroll 1
     for (int tile = tile0 - 1; tile < tile1; ++tile) {
@@ -592,7 +704,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         if (tile + 1 < tile1) make(tile + 1, sm + kTreeBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
         if (late) __syncthreads();
         const int at = late ? tile + 1 : tile;
-        if (at >= tile0 && at < tile1 && (TW <= 4 || tw < 4)) attend(at, sm + kTreeBuf + ((at - tile0) & 1) * kBufBytes);
+        if (at >= tile0 && at < tile1) attend(at, sm + kTreeBuf + ((at - tile0) & 1) * kBufBytes);
         if (!late) __syncthreads();
     }
     if constexpr (TW == 1) {
