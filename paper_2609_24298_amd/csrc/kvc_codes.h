@@ -32,26 +32,40 @@ __host__ __device__ constexpr int bt_coord(int p) {
     return 16 * (4 * (p >> 6) + (p & 3)) + ((p >> 2) & 15);
 }
 
-// Stages P^T (rows of P past the rank are zero, so codes past the rank meet zeros): a thread takes four
-// positions and eight features, lanes consecutive positions.
+// Stages P^T (rows of P past the rank are zero, so codes past the rank meet zeros): item e of (kD / 4) (kD / 8) is four
+// positions and eight features, consecutive items consecutive positions. Loads and stores apart, so that a kernel may request
+// the basis long before it has room for it.
+constexpr int kBtItems = (kD / 4) * (kD / 8);
+template <int side>
+__device__ __forceinline__ void basis_t_load(uint4 (&x)[4], const uint16_t* __restrict__ P, int r, int e) {
+    const int w = e & (kD / 4 - 1), f0 = 8 * (e / (kD / 4));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = bt_coord<side>(4 * w + j);
+        x[j] = i < r ? load_basis8(P + (int64_t)i * kD + f0) : uint4{0u, 0u, 0u, 0u};
+    }
+}
+__device__ __forceinline__ void basis_t_store(uint8_t* __restrict__ PT, const uint4 (&v)[4], int e) {
+    const int w = e & (kD / 4 - 1), f0 = 8 * (e / (kD / 4));
+    uint32_t x[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[j][0] = v[j].x; x[j][1] = v[j].y; x[j][2] = v[j].z; x[j][3] = v[j].w;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t sel = (k & 1) ? 0x07060302u : 0x05040100u;
+        const int f = f0 + k;
+        *reinterpret_cast<uint2*>(PT + bt_block(f >> 4, w >> 3) + bt_lane(f & 15, (w >> 1) & 3) + 8 * (w & 1)) =
+            uint2{perm(x[1][k >> 1], x[0][k >> 1], sel), perm(x[3][k >> 1], x[2][k >> 1], sel)};
+    }
+}
 template <int side>
 __device__ __forceinline__ void stage_basis_t(uint8_t* __restrict__ PT, const uint16_t* __restrict__ P, int r, int tid, int threads) {
-    for (int e = tid; e < (kD / 4) * (kD / 8); e += threads) {
-        const int w = e & (kD / 4 - 1), f0 = 8 * (e / (kD / 4));
-        uint32_t x[4][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = bt_coord<side>(4 * w + j);
-            const uint4 v = i < r ? load_basis8(P + (int64_t)i * kD + f0) : uint4{0u, 0u, 0u, 0u};
-            x[j][0] = v.x; x[j][1] = v.y; x[j][2] = v.z; x[j][3] = v.w;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t sel = (k & 1) ? 0x07060302u : 0x05040100u;
-            const int f = f0 + k;
-            *reinterpret_cast<uint2*>(PT + bt_block(f >> 4, w >> 3) + bt_lane(f & 15, (w >> 1) & 3) + 8 * (w & 1)) =
-                uint2{perm(x[1][k >> 1], x[0][k >> 1], sel), perm(x[3][k >> 1], x[2][k >> 1], sel)};
-        }
+    for (int e = tid; e < kBtItems; e += threads) {
+        uint4 x[4];
+        basis_t_load<side>(x, P, r, e);
+        basis_t_store(PT, x, e);
     }
 }
 

@@ -253,9 +253,15 @@ constexpr int kTreeAdv = kBtBytes, kTreeMid = kTreeAdv + (kD / 2) * 8;  // and t
 constexpr int kTreePRow = kD + 8;  // plain keys: P_K at 0 instead, in rows of this many elements
 constexpr int kTreeBuf = kD * kTreePRow * 2;
 static_assert(kTreeMid + kD * 4 <= kTreeBuf);
-constexpr int kBufLo = kTile * kD * 2, kBufV = kBufLo + kTile * kD, kBufBytes = kBufV + kTile * kD * 2;
-constexpr int kTreeLead = kTreeBuf + 2 * kBufBytes;  // the queries' leading bits: [wavefront][cb][2][lane]
-constexpr int tree_smem(int cb) { return kTreeLead + kTreeWaves * cb * 2048; }
+constexpr int kBufLo = kTile * kD * 2, kTreeBufV = kBufLo + kTile * kD, kTreeBufBytes = kTreeBufV + kTile * kD * 2;
+constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading bits: [wavefront][cb][2][lane]
+// Plain keys and up to 64 rows: two blocks share a CU, each with half its registers and LDS. (The basis lies in the buffers, the
+// projected queries' low parts behind them: [row block][4][lane].)
+constexpr bool tree_pair(int cb, int rw, bool rope) { return !rope && cb == 1 && rw <= 4; }
+constexpr int kPairLow = 2 * kTile * kD * 4;
+constexpr int tree_smem(int cb, int rw, bool rope) {
+    if (tree_pair(cb, rw, rope)) return kPairLow + rw * 4096;
+    return kTreeLead + kTreeWaves * cb * 2048; }
 
 // Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, the
 // wavefronts make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
@@ -270,6 +276,8 @@ template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
+    constexpr bool kPair = tree_pair(CB, RW, ROPE);
+    constexpr int kBuf = kPair ? 0 : kTreeBuf, kBufV = ROPE ? kTreeBufV : kTile * kD * 2, kBufBytes = ROPE ? kTreeBufBytes : kTile * kD * 4;
     constexpr int TW = kTreeWaves / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // opaque: a lane's addresses are formed again for every piece, not kept across all of them
@@ -310,94 +318,139 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         }
         if (wv < nvt) tree_v_load(vrs, tile * vtb, bv, va, vw);
     };
-    load(tile0);
-    // queries: columns of the operand. Rotated keys: features in the order of the rebuilt keys, and their leading bits.
-    // Plain keys: the projections onto the basis, in the order of the unpacked codes, as the sum of two fp16 (2^-22 of them)
-    constexpr int QW = ROPE ? 1 : 2;
-    uint8_t* lead = sm + kTreeLead + wv * CB * 2048 + lane * 16;
-    rc_h8 qf[QW][CB][4];
-    float base[CB];  // the centre's share of a row's raw products, -(2^(b-1) - 1/2) sum_i q_i
+    // The basis and the queries are requested first, then the first tile's codes.
+    constexpr int kBasisItems = kD * kD / 8 / kTreeThreads;
+    static_assert(kBasisItems == 4 && kBtItems == kTreeThreads);
+    const uint16_t* Pg = K.basis + K.basis_off[u];
+    uint4 pr[kBasisItems];
     if constexpr (ROPE) {
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const int row = row0 + 16 * cb + col;
-            const uint16_t* qr = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD + 4 * grp;
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                uint2 a = *reinterpret_cast<const uint2*>(qr + 32 * ks), b = *reinterpret_cast<const uint2*>(qr + 32 * ks + 16);
-                if (row >= wk.M) a = b = uint2{0u, 0u};
-                qf[0][cb][ks] = __builtin_bit_cast(rc_h8, v4u{a.x, a.y, b.x, b.y});
-            }
-            const v8i r = lead_bits(qf[0][cb]);  // for this wavefront alone
-            *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
-            *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
-            base[cb] = 0.f;
-        }
+        basis_t_load<KVC_SIDE_K>(pr, Pg, rk, tid);
     } else {
-        rc_h8 qr[CB][4];
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            const int row = row0 + 16 * cb + col;
-            const uint16_t* qp = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD + 8 * grp;
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks) {
-                uint4 a = *reinterpret_cast<const uint4*>(qp + 32 * ks);
-                if (row >= wk.M) a = uint4{0u, 0u, 0u, 0u};
-                qr[cb][ks] = __builtin_bit_cast(rc_h8, a);
-            }
-        }
-        // the basis, staged for all wavefronts (rows past the rank zero)
-        uint16_t* Pl = reinterpret_cast<uint16_t*>(sm);
-        const uint16_t* Pg = K.basis + K.basis_off[u];
-        uint4 pr[kD * kD / 8 / kTreeThreads];
-#pragma unroll
-        for (int j = 0; j < kD * kD / 8 / kTreeThreads; ++j) {
+        for (int j = 0; j < kBasisItems; ++j) {
             const int e = tid + j * kTreeThreads;
             pr[j] = uint4{0u, 0u, 0u, 0u};
             if (e < rk * (kD / 8)) pr[j] = load_basis8(Pg + 8 * e);
         }
+    }
+    // Queries: columns of the operand. Rotated keys: features in the order of the rebuilt keys, and their leading bits.
+    // Plain keys: the projections onto the basis, in the order of the unpacked codes, as the sum of two fp16 (2^-22 of them)
+    constexpr int QW = ROPE || kPair ? 1 : 2;  // parts held in registers
+    uint8_t* low = sm + kPairLow + rw * 4096 + lane * 16;
+    uint8_t* lead = sm + kTreeLead + wv * CB * 2048 + lane * 16;
+    rc_h8 qr[CB][4], qf[QW][CB][4];
+    float base[CB];  // the centre's share of a row's raw products, -(2^(b-1) - 1/2) sum_i q_i
 #pragma unroll
-        for (int j = 0; j < kD * kD / 8 / kTreeThreads; ++j) {
-            const int e = tid + j * kTreeThreads;
-            *reinterpret_cast<uint4*>(Pl + (e >> 4) * kTreePRow + 8 * (e & 15)) = pr[j];
+    for (int cb = 0; cb < CB; ++cb) {
+        const int row = row0 + 16 * cb + col;
+        const uint16_t* qp = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            uint4 x;
+            if constexpr (ROPE) {
+                const uint2 a = *reinterpret_cast<const uint2*>(qp + 4 * grp + 32 * ks), b = *reinterpret_cast<const uint2*>(qp + 4 * grp + 32 * ks + 16);
+                x = uint4{a.x, a.y, b.x, b.y};
+            } else {
+                x = *reinterpret_cast<const uint4*>(qp + 8 * grp + 32 * ks);
+            }
+            if (row >= wk.M) x = uint4{0u, 0u, 0u, 0u};
+            qr[cb][ks] = __builtin_bit_cast(rc_h8, x);
         }
-        __syncthreads();
+    }
+    load(tile0);
+    if constexpr (ROPE) {
+        basis_t_store(sm, pr, tid);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) qf[0][cb][ks] = qr[cb][ks];
+            const v8i r = lead_bits(qr[cb]);  // for this wavefront alone
+            *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
+            *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
+            base[cb] = 0.f;
+        }
+        if (tid < kD / 2) {
+            const double t = (double)kTile * rope.freq[tid];
+            const float f = (float)(t - rint(t));
+            adv[tid] = float2{__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f)};
+        }
+        __syncthreads();  // P_K^T
+        // the centre's share of a key, -(2^(b-1) - 1/2) sum_i P_i: features 16 wv + 4 grp + v, in every column
         const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
         const rc_h8 cc = {c, c, c, c, c, c, c, c};
-        rc_f4 sum[CB];
+        rc_f4 a = rc_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) sum[cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < 4; ++s) a = mfma_h(*reinterpret_cast<const rc_h8*>(sm + bt_block(wv, s) + bt_lane(col, grp)), cc, a);
+        if (col == 0) *reinterpret_cast<rc_f4*>(mid + 16 * wv + 4 * grp) = a * (1.f / kRawScale);
+        __syncthreads();
+    } else {
+        // Rows of P_K, eight features to a chunk; a row's chunks are turned by four for every sixteen rows, since a read takes
+        // rows i, i + 1, i + 2, i + 3 and those 16, 32 and 48 further.
+        uint16_t* Pl = reinterpret_cast<uint16_t*>(sm);
+        auto chunk = [&](int i, int c8) { return Pl + i * kTreePRow + 8 * ((c8 + 4 * (i >> 4)) & 15); };
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {  // coordinates 64 (ks / 2) + 16 grp + 4 (ks % 2) + v, and 8 further
-            rc_f4 d[2][CB];
+        for (int j = 0; j < kBasisItems; ++j) {
+            const int e = tid + j * kTreeThreads;
+            *reinterpret_cast<uint4*>(chunk(e >> 4, e & 15)) = pr[j];
+        }
+        __syncthreads();
+        // matrix step ks of the scores: coordinates 64 (ks / 2) + 16 grp + 4 (ks % 2) + v, and 8 further
+        auto project = [&](int ks, int cb, rc_h8& hi, rc_h8& lo) {
+            rc_f4 d[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int i = 64 * (ks >> 1) + 16 * (col >> 2) + 4 * (ks & 1) + (col & 3) + 8 * h;
-                rc_h8 p[4];
+                d[h] = rc_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int fs = 0; fs < 4; ++fs) p[fs] = *reinterpret_cast<const rc_h8*>(Pl + i * kTreePRow + 32 * fs + 8 * grp);
+                for (int fs = 0; fs < 4; ++fs) d[h] = mfma_h(*reinterpret_cast<const rc_h8*>(chunk(i, 4 * fs + grp)), qr[cb][fs], d[h]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = d[e & 1][e >> 1] * kPlainScale;
+                hi[e] = (_Float16)x;
+                lo[e] = (_Float16)(x - (float)hi[e]);
+            }
+        };
+        rc_h8 ql[CB][4];
+        if constexpr (kPair) {  // the wavefronts of the same rows share the steps (TW is 2 or 4), by way of the second buffer
+            uint8_t* high = sm + kPairLow - RW * 4096 + rw * 4096 + lane * 16;
+#pragma unroll 1
+            for (int ks = tw; ks < 2 * nk; ks += TW) {
+                rc_h8 hi, lo;
+                project(ks, 0, hi, lo);
+                *reinterpret_cast<rc_h8*>(high + 1024 * ks) = hi;
+                *reinterpret_cast<rc_h8*>(low + 1024 * ks) = lo;
+            }
+            __syncthreads();  // and P_K has been read: its place is the first tile's
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                qf[0][0][ks] = ql[0][ks] = rc_h8{};
+                if (ks < 2 * nk) {
+                    qf[0][0][ks] = *reinterpret_cast<const rc_h8*>(high + 1024 * ks);
+                    ql[0][ks] = *reinterpret_cast<const rc_h8*>(low + 1024 * ks);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) {
-                    d[h][cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int fs = 0; fs < 4; ++fs) d[h][cb] = mfma_h(p[fs], qr[cb][fs], d[h][cb]);
+                    project(ks, cb, qf[0][cb][ks], ql[cb][ks]);
+                    qf[QW - 1][cb][ks] = ql[cb][ks];
                 }
-            }
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = d[e & 1][cb][e >> 1] * kPlainScale;
-                    const _Float16 hi = (_Float16)x;
-                    qf[0][cb][ks][e] = hi;
-                    qf[QW - 1][cb][ks][e] = (_Float16)(x - (float)hi);
-                }
-                sum[cb] = mfma_h(cc, qf[0][cb][ks], sum[cb]);
-                sum[cb] = mfma_h(cc, qf[QW - 1][cb][ks], sum[cb]);
-            }
         }
+        const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
+        const rc_h8 cc = {c, c, c, c, c, c, c, c};
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) base[cb] = sum[cb][0] * (1.f / kRawScale);
+        for (int cb = 0; cb < CB; ++cb) {
+            rc_f4 sum = rc_f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                sum = mfma_h(cc, qf[0][cb][ks], sum);
+                sum = mfma_h(cc, ql[cb][ks], sum);
+            }
+            base[cb] = sum[0] * (1.f / kRawScale);
+        }
     }
     // step_K log2(e) / sqrt(128), and what scales a raw product
     const float qs = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f * (ROPE ? 1.f : kRawScale / kPlainScale);
@@ -578,16 +631,20 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 for (int cb = 0; cb < CB; ++cb) S[t][cb] = rc_f4{base[cb], base[cb], base[cb], base[cb]};
             auto part = [&](auto first) {  // matrix steps `first` and `first` + 1
                 constexpr int s0 = decltype(first)::value;
-                rc_h8 kf[2 * TB];
+                rc_h8 kf[2 * TB], lw[2];
+                if constexpr (kPair)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) lw[i] = *reinterpret_cast<const rc_h8*>(low + 1024 * (s0 + i));
 #pragma unroll
                 for (int i = 0; i < 2 * TB; ++i) kf[i] = *reinterpret_cast<const rc_h8*>(kr + 4096 * (s0 + i / TB) + 256 * (i % TB));
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < 2 * TB; ++i)
 #pragma unroll
-                    for (int w = 0; w < QW; ++w)
+                    for (int w = 0; w < 2; ++w)
 #pragma unroll
-                        for (int cb = 0; cb < CB; ++cb) S[i % TB][cb] = mfma_h(kf[i], qf[w][cb][s0 + i / TB], S[i % TB][cb]);
+                        for (int cb = 0; cb < CB; ++cb)
+                            S[i % TB][cb] = mfma_h(kf[i], kPair && w ? lw[i / TB] : qf[w && !kPair ? QW - 1 : 0][cb][s0 + i / TB], S[i % TB][cb]);
             };
             part(std::integral_constant<int, 0>());
             if (nk > 1) part(std::integral_constant<int, 2>());
@@ -604,9 +661,10 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         // ---- online softmax
         constexpr int NS = TB > 1 ? TB / 2 : 1;  // halves of a tile: one or two
         const uint8_t* vr = buf + kBufV + (tb0 >> 1) * 1024 + lane * 16;
-        rc_h8 vf[NV];  // N-tiles past the rank make rows that are not stored
+        constexpr int AV = kPair && NV > 4 ? 4 : NV;  // operands read ahead
+        rc_h8 vf[AV];  // N-tiles past the rank make rows that are not stored
 #pragma unroll
-        for (int n = 0; n < NV; ++n) vf[n] = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
+        for (int n = 0; n < AV; ++n) vf[n] = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
         float top[CB];
         bool raise = false;
 #pragma unroll
@@ -651,9 +709,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[cb], L[cb]);
         if constexpr (NS == 1) {
 #pragma unroll
-            for (int n = 0; n < NV; ++n)
+            for (int n = 0; n < NV; ++n) {
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n % AV], P[cb], O[n][cb]);
+                if (n + AV < NV) vf[n % AV] = *reinterpret_cast<const rc_h8*>(vr + (n + AV) * 2048);
+            }
         } else {
             float w1[CB][8];
             __builtin_amdgcn_sched_barrier(0);
@@ -678,33 +738,15 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
         }
     };
-    if constexpr (ROPE) {
-    stage_basis_t<KVC_SIDE_K>(sm, K.basis + K.basis_off[u], rk, tid, kTreeThreads);
-    if (tid < kD / 2) {
-        const double t = (double)kTile * rope.freq[tid];
-        const float f = (float)(t - rint(t));
-        adv[tid] = float2{__builtin_amdgcn_cosf(f), __builtin_amdgcn_sinf(f)};
-    }
-    __syncthreads();  // P_K^T
-    {   // the centre's share of a key, -(2^(b-1) - 1/2) sum_i P_i: features 16 wv + 4 grp + v, in every column
-        const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
-        const rc_h8 cc = {c, c, c, c, c, c, c, c};
-        rc_f4 a = rc_f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < 4; ++s) a = mfma_h(*reinterpret_cast<const rc_h8*>(sm + bt_block(wv, s) + bt_lane(col, grp)), cc, a);
-        if (col == 0) *reinterpret_cast<rc_f4*>(mid + 16 * wv + 4 * grp) = a * (1.f / kRawScale);
-    }
-    __syncthreads();
-    }
     const bool late = wv >= kTreeWaves / 2;
 #pragma unroll 1
     for (int tile = tile0 - 1; tile < tile1; ++tile) {
         // One wavefront of each SIMD makes the next tile and then attends to the current one, the other (late) the other way
         // round, so that the matrix and vector work of the two overlap: the late ones meet the barrier between the two.
-        if (tile + 1 < tile1) make(tile + 1, sm + kTreeBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
+        if (tile + 1 < tile1) make(tile + 1, sm + kBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
         if (late) __syncthreads();
         const int at = late ? tile + 1 : tile;
-        if (at >= tile0 && at < tile1) attend(at, sm + kTreeBuf + ((at - tile0) & 1) * kBufBytes);
+        if (at >= tile0 && at < tile1) attend(at, sm + kBuf + ((at - tile0) & 1) * kBufBytes);
         if (!late) __syncthreads();
     }
     if constexpr (TW == 1) {
@@ -720,10 +762,10 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     } else {  // the token parts meet in LDS (the tiles' buffers)
         static_assert(CB == 1, "token parts have sixteen rows a wavefront");
         constexpr int kPitch = kD + 4;
-        float* parts = reinterpret_cast<float*>(sm + kTreeBuf);             // [TW][16 RW][kPitch]
+        float* parts = reinterpret_cast<float*>(sm + kBuf);             // [TW][16 RW][kPitch]
         float* tops = parts + kTreeWaves * 16 * kPitch;                     // [TW][16 RW]
         float* sums = tops + kTreeWaves * 16;                               // [TW][16 RW]
-        static_assert((kTreeWaves * 16 * (kPitch + 2)) * 4 <= 2 * kBufBytes, "parts exceed the buffers");
+        static_assert((kTreeWaves * 16 * (kPitch + 2)) * 4 <= tree_smem(CB, RW, ROPE) - kBuf, "parts exceed the buffers");
         __syncthreads();  // the late wavefronts have read their last tile
         if (grp == 0) tops[16 * wv + col] = m[0];  // wavefronts are in the order (tw, rw)
         __syncthreads();
@@ -755,7 +797,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 }
 
 template <int CB, int RW, bool ROPE>
-__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void tree_partial_kernel(
+__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(tree_pair(CB, RW, ROPE) ? 4 : 2, tree_pair(CB, RW, ROPE) ? 4 : 2))) void tree_partial_kernel(
     DevSide K, DevSide V, const uint16_t* __restrict__ q, const int32_t* __restrict__ seq_len, TreeWork wk, TreeRope rope,
     float* __restrict__ acc_out, float2* __restrict__ ml_out) {
     const int rb = blockIdx.x % wk.nrb, b = blockIdx.x / wk.nrb;
@@ -884,6 +926,11 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
             qr[ks] = *reinterpret_cast<const uint4*>(qp + 32 * ks);
         }
     }
+    constexpr int kBt = kBtItems / kFinThreads;
+    uint4 bt[kBt][4];
+    if (tiles)
+#pragma unroll
+        for (int j = 0; j < kBt; ++j) basis_t_load<KVC_SIDE_K>(bt[j], V.basis + V.basis_off[u], rv, tid + j * kFinThreads);
     __syncthreads();
     // the threads of row mr merge its pieces, whose slots follow one another: maxima, sums, eight coordinates each
     const int mr = tid / (16 * CG), mi = tid % (16 * CG), mc = mi & 15, cg = mi >> 4;
@@ -920,7 +967,8 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
-        stage_basis_t<KVC_SIDE_K>(sm, V.basis + V.basis_off[u], rv, tid, kFinThreads);
+#pragma unroll
+        for (int j = 0; j < kBt; ++j) basis_t_store(sm, bt[j], tid + j * kFinThreads);
     }
 #pragma unroll
     for (int j = 0; j < kXv; ++j) {
@@ -1028,7 +1076,7 @@ struct TreeLayout {
     int64_t acc, ml, total;
 };
 
-TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G, int n_tok, int max_seq) {
+TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G, int n_tok, int max_seq, bool rope) {
     TreeLayout t;
     const int U = k->n_units, tiles = (max_seq + kTile - 1) / kTile;
     t.wk.M = n_tok * G;
@@ -1041,7 +1089,7 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.v_cap_tiles = (v->capacity + kTile - 1) / kTile;
     // One block for every CU (its LDS lets no second one in), as long as there are tiles for them.
     t.wk.U = U;
-    t.wk.n_blocks = (int)std::min<int64_t>(std::max(1, device_cus() / t.wk.nrb), (int64_t)U * (tiles ? tiles + start_cost(t.wk.M) : 0));
+    t.wk.n_blocks = (int)std::min<int64_t>(std::max(1, device_cus() * (tree_pair(t.cb, t.rw, rope) ? 2 : 1) / t.wk.nrb), (int64_t)U * (tiles ? tiles + start_cost(t.wk.M) : 0));
     const int64_t rows = t.wk.n_blocks ? ((int64_t)t.wk.n_blocks + U) * t.wk.M : 0;
     auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
     t.acc = 0;
@@ -1053,9 +1101,9 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
 template <int CB, int RW, bool ROPE>
 int launch_tree_as(dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V, const uint16_t* q, const int32_t* seq_len, const TreeWork& wk,
                    const TreeRope& rope, float* acc, float2* ml) {
-    const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, RW, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, tree_smem(CB));
+    const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, RW, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, tree_smem(CB, RW, ROPE));
     if (e != hipSuccess) return set_error(KVC_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(kTreeThreads), tree_smem(CB), st, K, V, q, seq_len, wk, rope, acc, ml);
+    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(kTreeThreads), tree_smem(CB, RW, ROPE), st, K, V, q, seq_len, wk, rope, acc, ml);
     return check_launch("kvc_tree_attn");
 }
 
@@ -1096,7 +1144,7 @@ using namespace kvc;
 extern "C" size_t kvc_tree_attn_workspace(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok, int32_t max_seq_len) {
     clear_error();
     if (tree_check(k, v, G, n_tok, max_seq_len)) return 0;
-    return (size_t)tree_layout(k, v, G, n_tok, max_seq_len).total;
+    return (size_t)tree_layout(k, v, G, n_tok, max_seq_len, false).total;
 }
 
 extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* q, int32_t G, int32_t n_tok,
@@ -1117,7 +1165,7 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
             return set_error(KVC_EINVAL, "kvc_tree_attn: xk, xv must be 16-byte aligned with stride a multiple of 8 and >= n_tok*d");
     if (!ws) return set_error(KVC_EINVAL, "kvc_tree_attn: null workspace");
     if (reinterpret_cast<uintptr_t>(ws) & 255) return set_error(KVC_EINVAL, "kvc_tree_attn: workspace not 256-byte aligned");
-    const TreeLayout t = tree_layout(k, v, G, n_tok, max_seq_len);
+    const TreeLayout t = tree_layout(k, v, G, n_tok, max_seq_len, rope_base != 0.f);
     if ((int64_t)ws_bytes < t.total)
         return set_error(KVC_ENOSPACE, "kvc_tree_attn: workspace %zu < %lld bytes", ws_bytes, (long long)t.total);
     float* acc = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + t.acc);
