@@ -244,6 +244,9 @@ __device__ __forceinline__ void tree_v_frag(const uint32_t (&w)[4], int b, uint3
     }
 }
 
+// Item of the staged basis for a thread: four threads read 64 consecutive bytes of a row.
+__device__ __forceinline__ int basis_item(int t) { return ((t & 3) | (t >> 7 << 2)) * (kD / 4) + (t >> 2 & 31); }
+
 // ---------------------------------------------------------------- cached tokens
 
 constexpr int kTreeWaves = 8;
@@ -324,7 +327,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const uint16_t* Pg = K.basis + K.basis_off[u];
     uint4 pr[kBasisItems];
     if constexpr (ROPE) {
-        basis_t_load<KVC_SIDE_K>(pr, Pg, rk, tid);
+        basis_t_load<KVC_SIDE_K>(pr, Pg, rk, basis_item(tid));
     } else {
 #pragma unroll
         for (int j = 0; j < kBasisItems; ++j) {
@@ -359,7 +362,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     }
     load(tile0);
     if constexpr (ROPE) {
-        basis_t_store(sm, pr, tid);
+        basis_t_store(sm, pr, basis_item(tid));
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
@@ -930,7 +933,7 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
     uint4 bt[kBt][4];
     if (tiles)
 #pragma unroll
-        for (int j = 0; j < kBt; ++j) basis_t_load<KVC_SIDE_K>(bt[j], V.basis + V.basis_off[u], rv, tid + j * kFinThreads);
+        for (int j = 0; j < kBt; ++j) basis_t_load<KVC_SIDE_K>(bt[j], V.basis + V.basis_off[u], rv, basis_item(tid + j * kFinThreads));
     __syncthreads();
     // the threads of row mr merge its pieces, whose slots follow one another: maxima, sums, eight coordinates each
     const int mr = tid / (16 * CG), mi = tid % (16 * CG), mc = mi & 15, cg = mi >> 4;
@@ -968,7 +971,7 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
 #pragma unroll
-        for (int j = 0; j < kBt; ++j) basis_t_store(sm, bt[j], tid + j * kFinThreads);
+        for (int j = 0; j < kBt; ++j) basis_t_store(sm, bt[j], basis_item(tid + j * kFinThreads));
     }
 #pragma unroll
     for (int j = 0; j < kXv; ++j) {
