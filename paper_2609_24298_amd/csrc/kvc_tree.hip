@@ -45,6 +45,13 @@ __device__ __forceinline__ v8i lead_bits(const rc_h8 (&q)[4]) {
     return r;
 }
 
+// Two values rounded to fp16 by one instruction (left to itself the compiler forms the value a second time for each half).
+__device__ __forceinline__ rc_h2 to_half2(float x, float y) {
+    uint32_t r;
+    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+    return __builtin_bit_cast(rc_h2, r);
+}
+
 // Four values, times 2^11, as bf8.
 typedef short s2v __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ s2v bf8_pairs(const float (&x)[4]) {
@@ -279,7 +286,7 @@ template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
-    constexpr bool kPair = tree_pair(CB, RW, ROPE);
+    constexpr bool kPair = tree_pair(CB, RW, ROPE), kKeep = ROPE && CB == 1 && RW <= 4;
     constexpr int kBuf = kPair ? 0 : kTreeBuf, kBufV = ROPE ? kTreeBufV : kTile * kD * 2, kBufBytes = ROPE ? kTreeBufBytes : kTile * kD * 4;
     constexpr int TW = kTreeWaves / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
@@ -478,6 +485,14 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const rc_h8 ones = {h1, h1, h1, h1, h1, h1, h1, h1};
     float cs[2][4], sn[2][4];  // of the lane's pairs 32 fh + 16 i + 4 grp + v at its token's position, times kRawScale
 
+    rc_h8 pk[4][4];
+    if constexpr (kKeep) {
+        const uint8_t* pt = sm + bt_lane(col, grp) + bt_block(2 * fh, 0);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pk[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s));
+    }
     // keys and values of a tile to a buffer; the codes of the tile after it are requested
     auto make = [&](int tile, uint8_t* buf) {
         if constexpr (ROPE) {
@@ -542,21 +557,20 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         }
         auto rebuild = [&](auto first) {  // matrix steps `first` and `first` + 1: eight operands in flight
             constexpr int s0 = decltype(first)::value;
-            rc_h8 pa[2][2], pb[2][2];
+            rc_h8 p[2][4];
+            if constexpr (!kKeep) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s0 + s));
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    pa[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i, s0 + s));
-                    pb[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + 4, s0 + s));
-                }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    a[i] = mfma_h(pa[s][i], z[s0 + s], a[i]);
-                    b[i] = mfma_h(pb[s][i], z[s0 + s], b[i]);
+                    a[i] = mfma_h(kKeep ? pk[s0 + s][i] : p[s][i], z[s0 + s], a[i]);
+                    b[i] = mfma_h(kKeep ? pk[s0 + s][i + 2] : p[s][i + 2], z[s0 + s], b[i]);
                 }
         };
         rebuild(std::integral_constant<int, 0>());
@@ -572,10 +586,17 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             for (int v = 0; v < 4; ++v) {
                 x[v] = fmaf(a[i][v], cs[i][v], -b[i][v] * sn[i][v]);
                 y[v] = fmaf(a[i][v], sn[i][v], b[i][v] * cs[i][v]);
-                hx[4 * i + v] = (_Float16)x[v];
-                hy[4 * i + v] = (_Float16)y[v];
-                x[v] = fmaf((float)hx[4 * i + v], m1, x[v]);
-                y[v] = fmaf((float)hy[4 * i + v], m1, y[v]);
+            }
+#pragma unroll
+            for (int v = 0; v < 4; v += 2) {
+                const rc_h2 h = to_half2(x[v], x[v + 1]), g = to_half2(y[v], y[v + 1]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    hx[4 * i + v + e] = h[e];
+                    hy[4 * i + v + e] = g[e];
+                    x[v + e] = fmaf((float)h[e], m1, x[v + e]);
+                    y[v + e] = fmaf((float)g[e], m1, y[v + e]);
+                }
             }
             lx[i] = __builtin_bit_cast(int, bf8_pairs(x));
             ly[i] = __builtin_bit_cast(int, bf8_pairs(y));
@@ -664,7 +685,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         // ---- online softmax
         constexpr int NS = TB > 1 ? TB / 2 : 1;  // halves of a tile: one or two
         const uint8_t* vr = buf + kBufV + (tb0 >> 1) * 1024 + lane * 16;
-        constexpr int AV = kPair && NV > 4 ? 4 : NV;  // operands read ahead
+        constexpr int AV = (kPair || kKeep) && NV > 4 ? 4 : NV;  // operands read ahead
         rc_h8 vf[AV];  // N-tiles past the rank make rows that are not stored
 #pragma unroll
         for (int n = 0; n < AV; ++n) vf[n] = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
