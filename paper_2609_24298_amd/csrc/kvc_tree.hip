@@ -308,24 +308,26 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const int g16 = rk >> 4, rho = rk & 15, nk = (rk + 63) >> 6, nvt = (rv + 15) >> 4;
     const int fh = wv & 1, kb = wv >> 1;  // the feature half and token block that the wavefront rebuilds
     const int ktok = 16 * (col >> 2) + tree_tok(bv, kb, col & 3);
-    constexpr int KU = ROPE ? 2 : 1;  // 64-coordinate parts of the keys' codes that a wavefront unpacks: all, or part fh
+    constexpr int KU = ROPE && !kKeep ? 2 : 1;  // 64-coordinate parts of the keys' codes that a wavefront unpacks: all, or part fh
     uint32_t xk[KU];
     PlaneAt ka[KU];
     uint32_t kw[KU][kFieldWords] = {}, vw[4] = {};
 #pragma unroll
     for (int ks = 0; ks < KU; ++ks) {
-        const int cg = 4 * (ROPE ? ks : fh) + grp;  // a group past the rank reads the first one (its columns of P_K^T are zero)
+        const int cg = 4 * (KU > 1 ? ks : fh) + grp;  // a group past the rank reads the first one (its columns of P_K^T are zero)
         xk[ks] = cg < g16 ? (uint32_t)(1024 * cg + 16 * ktok) : (cg == g16 && rho ? (uint32_t)(1024 * g16 + ktok * rho) : (uint32_t)(g16 ? 16 * ktok : rho * ktok));
         ka[ks] = tree_k_at(bk, rk, xk[ks]);
     }
     const PlaneAt va = tree_v_at(bv, rv, wv, col, grp);
-    auto load = [&](int tile) {
-        if constexpr (ROPE) {
+    auto load_k = [&](int tile) {
+        if constexpr (KU > 1) {
             tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
             if (nk > 1) tree_k_load(krs, tile * ktb, bk, ka[KU - 1], kw[KU - 1]);
         } else if (fh < nk) {
             tree_k_load(krs, tile * ktb, bk, ka[0], kw[0]);
         }
+    };
+    auto load_v = [&](int tile) {
         if (wv < nvt) tree_v_load(vrs, tile * vtb, bv, va, vw);
     };
     // The basis and the queries are requested first, then the first tile's codes.
@@ -367,7 +369,8 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             qr[cb][ks] = __builtin_bit_cast(rc_h8, x);
         }
     }
-    load(tile0);
+    load_k(tile0);
+    load_v(tile0);
     if constexpr (ROPE) {
         basis_t_store(sm, pr, basis_item(tid));
 #pragma unroll
@@ -493,8 +496,25 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int i = 0; i < 4; ++i) pk[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s));
     }
+    // kKeep: the wavefront's part of a tile's key codes to LDS, where P_K^T was, a tile before they are needed
+    auto unpack = [&](int tile) {
+        if (fh < nk) {
+            rc_h8 zz[2];
+            tree_k_frag(kw[0], bk, xk[0], zz);
+            uint8_t* dst = sm + ((tile - tile0) & 1) * 16384 + 8192 * fh + 1024 * kb + lane * 16;
+            *reinterpret_cast<rc_h8*>(dst) = zz[0];
+            *reinterpret_cast<rc_h8*>(dst + 4096) = zz[1];
+        }
+        if (tile + 1 < tile1) load_k(tile + 1);
+    };
+    if constexpr (kKeep) {
+        __syncthreads();  // P_K^T is in registers
+        unpack(tile0);
+        __syncthreads();
+    }
     // keys and values of a tile to a buffer; the codes of the tile after it are requested
     auto make = [&](int tile, uint8_t* buf) {
+        rc_h8 z[4], vz[2];
         if constexpr (ROPE) {
             if ((tile - tile0) % kTreeResync == 0) {
                 const double pos = (double)(tile * kTile + ktok);
@@ -521,8 +541,16 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                     }
             }
         }
-        rc_h8 z[4], vz[2];
-        if constexpr (ROPE) {
+        if constexpr (kKeep) {
+            const uint8_t* src = sm + ((tile - tile0) & 1) * 16384 + 1024 * kb + lane * 16;
+            z[0] = *reinterpret_cast<const rc_h8*>(src);
+            z[1] = *reinterpret_cast<const rc_h8*>(src + 4096);
+            if (nk > 1) {
+                z[2] = *reinterpret_cast<const rc_h8*>(src + 8192);
+                z[3] = *reinterpret_cast<const rc_h8*>(src + 12288);
+            }
+            if (tile + 1 < tile1) unpack(tile + 1);
+        } else if constexpr (ROPE) {
             rc_h8 zz[2];
             tree_k_frag(kw[0], bk, xk[0], zz);
             z[0] = zz[0];
@@ -544,7 +572,10 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + lane * 16) = vz[0];
             *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + 1024 + lane * 16) = vz[1];
         }
-        if (tile + 1 < tile1) load(tile + 1);
+        if (tile + 1 < tile1) {
+            if constexpr (!kKeep) load_k(tile + 1);
+            load_v(tile + 1);
+        }
         if constexpr (!ROPE) return;
         int po = bt_lane(col, grp) + bt_block(2 * fh, 0);
         asm volatile("" : "+v"(po));  // opaque: P_K^T is read again for every tile and takes no registers in between
