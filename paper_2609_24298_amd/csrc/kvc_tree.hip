@@ -264,14 +264,15 @@ constexpr int kTreePRow = kD + 8;  // plain keys: P_K at 0 instead, in rows of t
 constexpr int kTreeBuf = kD * kTreePRow * 2;
 static_assert(kTreeMid + kD * 4 <= kTreeBuf);
 constexpr int kBufLo = kTile * kD * 2, kTreeBufV = kBufLo + kTile * kD, kTreeBufBytes = kTreeBufV + kTile * kD * 2;
-constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading bits: [wavefront][cb][2][lane]
+constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading bits, [wavefront][cb][2][lane], or two tiles' key codes
 // Plain keys and up to 64 rows: two blocks share a CU, each with half its registers and LDS. (The basis lies in the buffers, the
 // projected queries' low parts behind them: [row block][4][lane].)
 constexpr bool tree_pair(int cb, int rw, bool rope) { return !rope && cb == 1 && rw <= 4; }
 constexpr int kPairLow = 2 * kTile * kD * 4;
 constexpr int tree_smem(int cb, int rw, bool rope) {
     if (tree_pair(cb, rw, rope)) return kPairLow + rw * 4096;
-    return kTreeLead + kTreeWaves * cb * 2048; }
+    return kTreeLead + (cb == 2 ? kTreeWaves * cb * 2048 : 2 * kTile * kD * 2);
+}
 
 // Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, the
 // wavefronts make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
@@ -286,7 +287,8 @@ template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
-    constexpr bool kPair = tree_pair(CB, RW, ROPE), kKeep = ROPE && CB == 1 && RW <= 4;
+    constexpr bool kPair = tree_pair(CB, RW, ROPE), kShare = ROPE && CB == 1, kKeep = kShare && RW <= 4;
+    constexpr int kCodes = kKeep ? 0 : kTreeLead;  // kShare: two tiles' unpacked key codes
     constexpr int kBuf = kPair ? 0 : kTreeBuf, kBufV = ROPE ? kTreeBufV : kTile * kD * 2, kBufBytes = ROPE ? kTreeBufBytes : kTile * kD * 4;
     constexpr int TW = kTreeWaves / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
@@ -308,7 +310,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const int g16 = rk >> 4, rho = rk & 15, nk = (rk + 63) >> 6, nvt = (rv + 15) >> 4;
     const int fh = wv & 1, kb = wv >> 1;  // the feature half and token block that the wavefront rebuilds
     const int ktok = 16 * (col >> 2) + tree_tok(bv, kb, col & 3);
-    constexpr int KU = ROPE && !kKeep ? 2 : 1;  // 64-coordinate parts of the keys' codes that a wavefront unpacks: all, or part fh
+    constexpr int KU = ROPE && !kShare ? 2 : 1;  // 64-coordinate parts of the keys' codes that a wavefront unpacks: all, or part fh
     uint32_t xk[KU];
     PlaneAt ka[KU];
     uint32_t kw[KU][kFieldWords] = {}, vw[4] = {};
@@ -351,6 +353,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     uint8_t* low = sm + kPairLow + rw * 4096 + lane * 16;
     uint8_t* lead = sm + kTreeLead + wv * CB * 2048 + lane * 16;
     rc_h8 qr[CB][4], qf[QW][CB][4];
+    v8i q1 = {};
     float base[CB];  // the centre's share of a row's raw products, -(2^(b-1) - 1/2) sum_i q_i
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -377,9 +380,13 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) qf[0][cb][ks] = qr[cb][ks];
-            const v8i r = lead_bits(qr[cb]);  // for this wavefront alone
-            *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
-            *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
+            const v8i r = lead_bits(qr[cb]);
+            if constexpr (CB == 1) {
+                q1 = r;
+            } else {  // for this wavefront alone
+                *reinterpret_cast<v4i*>(lead + cb * 2048) = v4i{r[0], r[1], r[2], r[3]};
+                *reinterpret_cast<v4i*>(lead + cb * 2048 + 1024) = v4i{r[4], r[5], r[6], r[7]};
+            }
             base[cb] = 0.f;
         }
         if (tid < kD / 2) {
@@ -501,14 +508,14 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         if (fh < nk) {
             rc_h8 zz[2];
             tree_k_frag(kw[0], bk, xk[0], zz);
-            uint8_t* dst = sm + ((tile - tile0) & 1) * 16384 + 8192 * fh + 1024 * kb + lane * 16;
+            uint8_t* dst = sm + kCodes + ((tile - tile0) & 1) * 16384 + 8192 * fh + 1024 * kb + lane * 16;
             *reinterpret_cast<rc_h8*>(dst) = zz[0];
             *reinterpret_cast<rc_h8*>(dst + 4096) = zz[1];
         }
         if (tile + 1 < tile1) load_k(tile + 1);
     };
-    if constexpr (kKeep) {
-        __syncthreads();  // P_K^T is in registers
+    if constexpr (kShare) {
+        if constexpr (kKeep) __syncthreads();  // P_K^T is in registers
         unpack(tile0);
         __syncthreads();
     }
@@ -541,8 +548,8 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                     }
             }
         }
-        if constexpr (kKeep) {
-            const uint8_t* src = sm + ((tile - tile0) & 1) * 16384 + 1024 * kb + lane * 16;
+        if constexpr (kShare) {
+            const uint8_t* src = sm + kCodes + ((tile - tile0) & 1) * 16384 + 1024 * kb + lane * 16;
             z[0] = *reinterpret_cast<const rc_h8*>(src);
             z[1] = *reinterpret_cast<const rc_h8*>(src + 4096);
             if (nk > 1) {
@@ -573,7 +580,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             *reinterpret_cast<rc_h8*>(buf + kBufV + wv * 2048 + 1024 + lane * 16) = vz[1];
         }
         if (tile + 1 < tile1) {
-            if constexpr (!kKeep) load_k(tile + 1);
+            if constexpr (!kShare) load_k(tile + 1);
             load_v(tile + 1);
         }
         if constexpr (!ROPE) return;
@@ -658,8 +665,12 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             v8i q8[CB];
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                const v4i a = *reinterpret_cast<const v4i*>(lead + cb * 2048), b = *reinterpret_cast<const v4i*>(lead + cb * 2048 + 1024);
-                q8[cb] = v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                if constexpr (CB == 1) {
+                    q8[cb] = q1;
+                } else {
+                    const v4i a = *reinterpret_cast<const v4i*>(lead + cb * 2048), b = *reinterpret_cast<const v4i*>(lead + cb * 2048 + 1024);
+                    q8[cb] = v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
