@@ -812,7 +812,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         if (tile + 1 < tile1) make(tile + 1, sm + kBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
         if (late) __syncthreads();
         const int at = late ? tile + 1 : tile;
-        if (at >= tile0 && at < tile1) attend(at, sm + kBuf + ((at - tile0) & 1) * kBufBytes);
+        if (at >= tile0 && at < tile1 && row0 < wk.M) attend(at, sm + kBuf + ((at - tile0) & 1) * kBufBytes);
         if (!late) __syncthreads();
     }
     if constexpr (TW == 1) {
