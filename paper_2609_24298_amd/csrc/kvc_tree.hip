@@ -936,11 +936,11 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
                                                                   const uint16_t* __restrict__ xk, int64_t xk_stride,
                                                                   const uint16_t* __restrict__ xv, int64_t xv_stride,
                                                                   const uint64_t* __restrict__ mask, const int32_t* __restrict__ seq_len,
-                                                                  TreeWork wk, const float* __restrict__ acc, const float2* __restrict__ ml,
-                                                                  uint16_t* __restrict__ out) {
+                                                                  TreeWork wk, int groups, const float* __restrict__ acc,
+                                                                  const float2* __restrict__ ml, uint16_t* __restrict__ out) {
     constexpr int CG = 16 / R;  // threads of a row: CG x 16, eight coordinates each, every CG-th piece
-    const int nfb = (wk.M + R - 1) / R;
-    const int u = blockIdx.x / nfb, row0 = blockIdx.x % nfb * R;
+    const int nfb = (wk.M + groups * R - 1) / (groups * R);
+    const int u = blockIdx.x / nfb, row_lo = blockIdx.x % nfb * groups * R, row_hi = min(wk.M, row_lo + groups * R);
     const int tid = threadIdx.x, wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
     uint8_t* sm = kvc_dsm;
     float* zs = reinterpret_cast<float*>(sm + kFinZ);
@@ -951,9 +951,7 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
     float* inv = big + 16;
     uint32_t* count = reinterpret_cast<uint32_t*>(sm + kFinCount);  // tiles of all units and of those before u, by wavefront
     const int rv = uni(V.r[u]);
-    const int row = min(row0 + min(col, R - 1), wk.M - 1);
     const uint64_t live = n_tok == 64 ? ~0ull : (1ull << n_tok) - 1ull;
-    const uint64_t mine = mask[(int64_t)u * n_tok + row / G] & live;
     // Everything that the block reads is requested as early as its address is known.
     uint64_t named = lane < n_tok ? mask[(int64_t)u * n_tok + lane] & live : 0ull;
     int tiles = 0;
@@ -979,17 +977,15 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         xr[j] = uint4{0u, 0u, 0u, 0u};
         if ((named >> t) & 1) xr[j] = *reinterpret_cast<const uint4*>(xv + (int64_t)u * xv_stride + (int64_t)t * kD + 8 * c8);
     }
-    uint4 kr[4], qr[4];  // the wavefront's sixteen drafted tokens, the block's rows
+    uint4 kr[4];  // the wavefront's sixteen drafted tokens
     {
         const int t = 16 * wv + col;
         const bool there = (named >> t) & 1;
         const uint16_t* kp = xk + (int64_t)u * xk_stride + (int64_t)t * kD + 8 * grp;
-        const uint16_t* qp = q + ((int64_t)u * wk.M + row) * kD + 8 * grp;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
             kr[ks] = uint4{0u, 0u, 0u, 0u};
             if (there) kr[ks] = *reinterpret_cast<const uint4*>(kp + 32 * ks);
-            qr[ks] = *reinterpret_cast<const uint4*>(qp + 32 * ks);
         }
     }
     constexpr int kBt = kBtItems / kFinThreads;
@@ -997,141 +993,159 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
     if (tiles)
 #pragma unroll
         for (int j = 0; j < kBt; ++j) basis_t_load<KVC_SIDE_K>(bt[j], V.basis + V.basis_off[u], rv, basis_item(tid + j * kFinThreads));
+    uint4 qr[4];  // a group's rows
+    uint64_t mine;
+    auto rows = [&](int row0) {
+        const int row = min(row0 + min(col, R - 1), wk.M - 1);
+        const uint16_t* qp = q + ((int64_t)u * wk.M + row) * kD + 8 * grp;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) qr[ks] = *reinterpret_cast<const uint4*>(qp + 32 * ks);
+        mine = mask[(int64_t)u * n_tok + row / G] & live;
+    };
+    rows(row_lo);
     __syncthreads();
-    // the threads of row mr merge its pieces, whose slots follow one another: maxima, sums, eight coordinates each
-    const int mr = tid / (16 * CG), mi = tid % (16 * CG), mc = mi & 15, cg = mi >> 4;
-    const int mrow = min(row0 + mr, wk.M - 1);
-    float Mp = -INFINITY, l = 0.f;
-    float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (tiles) {
-        const uint32_t before = (count[4] + count[5]) + (count[6] + count[7]) + start_cost(wk.M);
-        const uint32_t per = run_tiles((count[0] + count[1]) + (count[2] + count[3]), wk.n_blocks);
-        const uint32_t b0 = before / per;
-        const int64_t slot0 = (int64_t)b0 + u;
-        const int n_pieces = (int)((before + (uint32_t)tiles - 1u) / per - b0) + 1;
-        const float2* mlr = ml + slot0 * wk.M + mrow;
-        const bool have = 8 * mc < ((rv + 15) & ~15);
-        const float* ar = acc + (slot0 * wk.M + mrow) * kD + (have ? 8 * mc : 0);
-        const int64_t stride = (int64_t)wk.M * kD;
-        for (int c = mi; c < n_pieces; c += 16 * CG) Mp = fmaxf(Mp, mlr[(int64_t)c * wk.M].x);
-#pragma unroll
-        for (int o = 1; o < 16 * CG; o <<= 1) Mp = fmaxf(Mp, __shfl_xor(Mp, o));
-#pragma unroll 4
-        for (int c = cg; c < n_pieces; c += CG) {
-            const float2 v = mlr[(int64_t)c * wk.M];
-            const float4 a = *reinterpret_cast<const float4*>(ar + c * stride), b = *reinterpret_cast<const float4*>(ar + c * stride + 4);
-            const float w = __builtin_amdgcn_exp2f(v.x - Mp);
-            l = fmaf(w, v.y, l);
-            z[0] = fmaf(w, a.x, z[0]); z[1] = fmaf(w, a.y, z[1]); z[2] = fmaf(w, a.z, z[2]); z[3] = fmaf(w, a.w, z[3]);
-            z[4] = fmaf(w, b.x, z[4]); z[5] = fmaf(w, b.y, z[5]); z[6] = fmaf(w, b.z, z[6]); z[7] = fmaf(w, b.w, z[7]);
-        }
-#pragma unroll
-        for (int o = 16; o < 16 * CG; o <<= 1) {
-            l += __shfl_xor(l, o);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] += __shfl_xor(z[e], o);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
-#pragma unroll
-        for (int j = 0; j < kBt; ++j) basis_t_store(sm, bt[j], basis_item(tid + j * kFinThreads));
-    }
-#pragma unroll
-    for (int j = 0; j < kXv; ++j) {
-        const int e = tid + j * kFinThreads;
-        *reinterpret_cast<uint4*>(xs + (e >> 4) * kFinXPitch + 8 * (e & 15)) = xr[j];
-    }
-    // scores of the drafted tokens (rows of the result) and the block's rows (columns)
-    float s[4];
-    {
-        rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) c = mfma_h(__builtin_bit_cast(rc_h8, kr[ks]), __builtin_bit_cast(rc_h8, qr[ks]), c);
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            s[v] = (mine >> (16 * wv + 4 * grp + v)) & 1 ? c[v] * (1.4426950408889634f * 0.08838834764831845f) : -INFINITY;
-    }
-    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (grp == 0) red[wv * 16 + col] = top;
-    __syncthreads();
-    float M = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
-    M = fmaxf(M, Mp);
-    const float Mf = M == -INFINITY ? 0.f : M;
-    {
-        const float w = __builtin_amdgcn_exp2f(Mp - Mf);
-        l *= w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] *= w;
-    }
-    if (mi == 0) big[mr] = Mf;
-    __syncthreads();
-    {
-        const float Mc = big[min(col, R - 1)];
-        float sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const _Float16 h = (_Float16)__builtin_amdgcn_exp2f(s[v] - Mc);
-            ps[col * kFinPPitch + 16 * wv + 4 * grp + v] = h;
-            sum += (float)h;
-        }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (grp == 0) red[64 + wv * 16 + col] = sum;
-    }
-    __syncthreads();
-    {
-        const float sum = l + ((red[64 + mr] + red[80 + mr]) + (red[96 + mr] + red[112 + mr]));
-        const float i = sum > 0.f ? 1.f / sum : 0.f;
-        if (mi == 0) inv[mr] = i;
-        if (cg == 0)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) zs[mr * kFinZPitch + 8 * mc + e] = z[e] * i;
-    }
-    __syncthreads();
-    const int zc = min(col, R - 1);
-    const float step = V.delta[u], rinv = inv[zc];
-    rc_f4 o[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int rb = 2 * wv + i;
-        rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f}, t = c;
+    int row0 = row_lo;
+    do {
+        // the threads of row mr merge its pieces, whose slots follow one another: maxima, sums, eight coordinates each
+        const int mr = tid / (16 * CG), mi = tid % (16 * CG), mc = mi & 15, cg = mi >> 4;
+        const int mrow = min(row0 + mr, wk.M - 1);
+        float Mp = -INFINITY, l = 0.f;
+        float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (tiles) {
+            const uint32_t before = (count[4] + count[5]) + (count[6] + count[7]) + start_cost(wk.M);
+            const uint32_t per = run_tiles((count[0] + count[1]) + (count[2] + count[3]), wk.n_blocks);
+            const uint32_t b0 = before / per;
+            const int64_t slot0 = (int64_t)b0 + u;
+            const int n_pieces = (int)((before + (uint32_t)tiles - 1u) / per - b0) + 1;
+            const float2* mlr = ml + slot0 * wk.M + mrow;
+            const bool have = 8 * mc < ((rv + 15) & ~15);
+            const float* ar = acc + (slot0 * wk.M + mrow) * kD + (have ? 8 * mc : 0);
+            const int64_t stride = (int64_t)wk.M * kD;
+            for (int c = mi; c < n_pieces; c += 16 * CG) Mp = fmaxf(Mp, mlr[(int64_t)c * wk.M].x);
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                rc_h8 hi, lo;
+            for (int o = 1; o < 16 * CG; o <<= 1) Mp = fmaxf(Mp, __shfl_xor(Mp, o));
+#pragma unroll 4
+            for (int c = cg; c < n_pieces; c += CG) {
+                const float2 v = mlr[(int64_t)c * wk.M];
+                const float4 a = *reinterpret_cast<const float4*>(ar + c * stride), b = *reinterpret_cast<const float4*>(ar + c * stride + 4);
+                const float w = __builtin_amdgcn_exp2f(v.x - Mp);
+                l = fmaf(w, v.y, l);
+                z[0] = fmaf(w, a.x, z[0]); z[1] = fmaf(w, a.y, z[1]); z[2] = fmaf(w, a.z, z[2]); z[3] = fmaf(w, a.w, z[3]);
+                z[4] = fmaf(w, b.x, z[4]); z[5] = fmaf(w, b.y, z[5]); z[6] = fmaf(w, b.z, z[6]); z[7] = fmaf(w, b.w, z[7]);
+            }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = zs[zc * kFinZPitch + bt_coord<KVC_SIDE_K>(32 * st) + 16 * grp + (e >> 1) + 8 * (e & 1)];
-                    const _Float16 h = (_Float16)x;
-                    hi[e] = h;
-                    lo[e] = (_Float16)(x - (float)h);
-                }
-                const rc_h8 p = *reinterpret_cast<const rc_h8*>(sm + bt_block(rb, st) + bt_lane(col, grp));
-                c = mfma_h(p, hi, c);
-                c = mfma_h(p, lo, c);
+            for (int o = 16; o < 16 * CG; o <<= 1) {
+                l += __shfl_xor(l, o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] += __shfl_xor(z[e], o);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
+        }
+        if (row0 == row_lo) {
+            if (tiles)
+#pragma unroll
+                for (int j = 0; j < kBt; ++j) basis_t_store(sm, bt[j], basis_item(tid + j * kFinThreads));
+#pragma unroll
+            for (int j = 0; j < kXv; ++j) {
+                const int e = tid + j * kFinThreads;
+                *reinterpret_cast<uint4*>(xs + (e >> 4) * kFinXPitch + 8 * (e & 15)) = xr[j];
             }
         }
+        // scores of the drafted tokens (rows of the result) and the block's rows (columns)
+        float s[4];
+        {
+            rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            rc_h8 a, b;
+            for (int ks = 0; ks < 4; ++ks) c = mfma_h(__builtin_bit_cast(rc_h8, kr[ks]), __builtin_bit_cast(rc_h8, qr[ks]), c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = xs[(32 * st + 8 * grp + e) * kFinXPitch + 16 * rb + col];
-            b = *reinterpret_cast<const rc_h8*>(ps + col * kFinPPitch + 32 * st + 8 * grp);
-            t = mfma_h(a, b, t);
+            for (int v = 0; v < 4; ++v)
+                s[v] = (mine >> (16 * wv + 4 * grp + v)) & 1 ? c[v] * (1.4426950408889634f * 0.08838834764831845f) : -INFINITY;
         }
+        if (R == kFinRows && row0 + R < row_hi) rows(row0 + R);
+        float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (grp == 0) red[wv * 16 + col] = top;
+        __syncthreads();
+        float M = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
+        M = fmaxf(M, Mp);
+        const float Mf = M == -INFINITY ? 0.f : M;
+        {
+            const float w = __builtin_amdgcn_exp2f(Mp - Mf);
+            l *= w;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) o[i][v] = fmaf(c[v], step, t[v] * rinv);
-    }
-    if (col < R && row0 + col < wk.M) {
+            for (int e = 0; e < 8; ++e) z[e] *= w;
+        }
+        if (mi == 0) big[mr] = Mf;
+        __syncthreads();
+        {
+            const float Mc = big[min(col, R - 1)];
+            float sum = 0.f;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const _Float16 h = (_Float16)__builtin_amdgcn_exp2f(s[v] - Mc);
+                ps[col * kFinPPitch + 16 * wv + 4 * grp + v] = h;
+                sum += (float)h;
+            }
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (grp == 0) red[64 + wv * 16 + col] = sum;
+        }
+        __syncthreads();
+        {
+            const float sum = l + ((red[64 + mr] + red[80 + mr]) + (red[96 + mr] + red[112 + mr]));
+            const float i = sum > 0.f ? 1.f / sum : 0.f;
+            if (mi == 0) inv[mr] = i;
+            if (cg == 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) zs[mr * kFinZPitch + 8 * mc + e] = z[e] * i;
+        }
+        __syncthreads();
+        const int zc = min(col, R - 1);
+        const float step = V.delta[u], rinv = inv[zc];
+        rc_f4 o[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-            const h4 h = {(_Float16)o[i][0], (_Float16)o[i][1], (_Float16)o[i][2], (_Float16)o[i][3]};
-            *reinterpret_cast<h4*>(out + ((int64_t)u * wk.M + row0 + col) * kD + 16 * (2 * wv + i) + 4 * grp) = h;
+            const int rb = 2 * wv + i;
+            rc_f4 c = rc_f4{0.f, 0.f, 0.f, 0.f}, t = c;
+            if (tiles) {
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    rc_h8 hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = zs[zc * kFinZPitch + bt_coord<KVC_SIDE_K>(32 * st) + 16 * grp + (e >> 1) + 8 * (e & 1)];
+                        const _Float16 h = (_Float16)x;
+                        hi[e] = h;
+                        lo[e] = (_Float16)(x - (float)h);
+                    }
+                    const rc_h8 p = *reinterpret_cast<const rc_h8*>(sm + bt_block(rb, st) + bt_lane(col, grp));
+                    c = mfma_h(p, hi, c);
+                    c = mfma_h(p, lo, c);
+                }
+            }
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                rc_h8 a, b;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = xs[(32 * st + 8 * grp + e) * kFinXPitch + 16 * rb + col];
+                b = *reinterpret_cast<const rc_h8*>(ps + col * kFinPPitch + 32 * st + 8 * grp);
+                t = mfma_h(a, b, t);
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[i][v] = fmaf(c[v], step, t[v] * rinv);
         }
-    }
+        if (col < R && row0 + col < wk.M) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+                const h4 h = {(_Float16)o[i][0], (_Float16)o[i][1], (_Float16)o[i][2], (_Float16)o[i][3]};
+                *reinterpret_cast<h4*>(out + ((int64_t)u * wk.M + row0 + col) * kD + 16 * (2 * wv + i) + 4 * grp) = h;
+            }
+        }
+        row0 += R;
+    } while (R == kFinRows && row0 < row_hi);  // (smaller groups come one to a block)
 }
 
 // ---------------------------------------------------------------- host side
@@ -1240,7 +1254,10 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     const DevSide K = dev_side(k), V = dev_side(v);
     const int64_t blocks = (int64_t)t.wk.nrb * t.wk.n_blocks;
     const int R = (int64_t)k->n_units * ((t.wk.M + 15) / 16) < device_cus() / 2 ? 4 : 16;
-    const int64_t fin = (int64_t)k->n_units * ((t.wk.M + R - 1) / R);
+    // A block takes as many groups of R rows, one after another, as it takes to have no second turn of blocks (two fit a CU).
+    const int64_t all_groups = (int64_t)k->n_units * ((t.wk.M + R - 1) / R), turn = 2 * (int64_t)device_cus();
+    const int groups = (int)std::min<int64_t>((t.wk.M + R - 1) / R, (all_groups + turn - 1) / turn);
+    const int64_t fin = (int64_t)k->n_units * ((t.wk.M + groups * R - 1) / (groups * R));
     if (blocks > INT32_MAX || fin > INT32_MAX) return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: too many units");
     if (blocks) {
         TreeRope rope;
@@ -1254,9 +1271,9 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     const dim3 grid((unsigned)fin), blk(kFinThreads);
     if (R == 4)
         hipLaunchKernelGGL(tree_finish_kernel<4>, grid, blk, kFinSmem, st, V, q, G, n_tok, xk, xk_unit_stride, xv, xv_unit_stride, mask, seq_len,
-                           t.wk, acc, ml, out);
+                           t.wk, groups, acc, ml, out);
     else
         hipLaunchKernelGGL(tree_finish_kernel<16>, grid, blk, kFinSmem, st, V, q, G, n_tok, xk, xk_unit_stride, xv, xv_unit_stride, mask, seq_len,
-                           t.wk, acc, ml, out);
+                           t.wk, groups, acc, ml, out);
     return check_launch("kvc_tree_attn");
 }
