@@ -3,9 +3,17 @@
 //
 // Rows (drafted token n, head g) of a unit, up to 1024 of them, share its keys, so that unlike a single
 // query's decode the products are dense: S^T = K Q^T and O^T = Z_V^T P^T with the rows as columns. Two kernels:
-//  tree_partial_kernel  the cached tokens, split over row blocks and context chunks: partials (m, l, O in the
-//                       rank space of the values) per row and chunk;
-//  tree_finish_kernel   per sixteen rows: merges the chunks, applies P_V, adds the drafted tokens.
+//  tree_partial_kernel  the cached tokens, all units' tiles cut into equal runs: per row and piece of a run (m, l, O in the
+//                       rank space of the values);
+//  tree_finish_kernel   per sixteen (or four) rows: merges the pieces, applies P_V, adds the drafted tokens.
+//
+// What bounds it (2 bits per dimension, 64 units of ragged lengths unless said, times of both kernels):
+//  256 rows x 32k  321 us, 667 TFLOP/s of score and value products: the vector unit (58 % of the time at work: rotation,
+//                  splitting, exponentials) beside the matrix units (40 %), which two wavefronts a SIMD overlap only in part.
+//   64 rows x 128k, 8 units at 1/2 bit  127 us: making the keys, which costs the same for one row or 64.
+//   52 rows x 16k, keys not rotated  75 us: LDS, at 190 KB a tile, and the latency of a tile's steps.
+//   20 rows x 300  17 us: two launches of about 8 us, a chain of four reads of memory each.
+// (The bytes, at most 110 MB a call, are never the bound.)
 #define KVC_DECODE_PARTIALS_UNIT
 #include "kvc_decode.hip"
 
@@ -266,7 +274,8 @@ static_assert(kTreeMid + kD * 4 <= kTreeBuf);
 constexpr int kBufLo = kTile * kD * 2, kTreeBufV = kBufLo + kTile * kD, kTreeBufBytes = kTreeBufV + kTile * kD * 2;
 constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading bits, [wavefront][cb][2][lane], or two tiles' key codes
 // Plain keys and up to 64 rows: two blocks share a CU, each with half its registers and LDS. (The basis lies in the buffers, the
-// projected queries' low parts behind them: [row block][4][lane].)
+// projected queries' low parts behind them: [row block][4][lane].) 32 rows x 32k x 64 units 122 -> 95 us, 64 rows x 128k x 8
+// units at 1/2 bit 83 -> 68, 52 rows x 16k x 64 units 79.7 and 79.9 (then 75 by sharing the projection).
 constexpr bool tree_pair(int cb, int rw, bool rope) { return !rope && cb == 1 && rw <= 4; }
 constexpr int kPairLow = 2 * kTile * kD * 4;
 constexpr int tree_smem(int cb, int rw, bool rope) {
@@ -283,12 +292,20 @@ constexpr int tree_smem(int cb, int rw, bool rope) {
 // A rotated key is fp16 and the rest of it bf8 at 2^11 times its size, met by the queries' leading bits (e5m2 is fp16's upper byte):
 // logits keep about 14 bits of the key for a quarter more matrix work, where fp16 alone would put an error of 2^-12 of
 // each coordinate into the weights.
+// Keys that are not rotated are not rebuilt: q . k = (P_K q) . z up to the step, so a piece begins by projecting its queries (kept
+// as the sum of two fp16, 2^-22 off), a wavefront makes tile t + 1 by unpacking half of a token block's codes, and the
+// products are of codes and projections. Twice the matrix steps for the scores, but the making is a quarter: 52 rows x 16k
+// x 64 units 115 us rebuilt, 78 so; 256 rows x 32k 335 and 274.
+// NV: N-tiles of values, so that ranks up to 64 and 96 do no products for the rest.
 template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
     constexpr bool kPair = tree_pair(CB, RW, ROPE), kShare = ROPE && CB == 1, kKeep = kShare && RW <= 4;
-    constexpr int kCodes = kKeep ? 0 : kTreeLead;  // kShare: two tiles' unpacked key codes
+    // kShare: the two wavefronts of a token block unpack half of its key codes each, a tile ahead, and meet in LDS (64 rows x 128k
+    // 134 -> 126 us, 100 rows x 16k 140 -> 136; with 32 rows a wavefront LDS has no room). kKeep: P_K^T stays in registers
+    // (138 -> 135; more rows leave no room).
+    constexpr int kCodes = kKeep ? 0 : kTreeLead;  // where two tiles' unpacked key codes are
     constexpr int kBuf = kPair ? 0 : kTreeBuf, kBufV = ROPE ? kTreeBufV : kTile * kD * 2, kBufBytes = ROPE ? kTreeBufBytes : kTile * kD * 4;
     constexpr int TW = kTreeWaves / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
@@ -503,7 +520,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int i = 0; i < 4; ++i) pk[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s));
     }
-    // kKeep: the wavefront's part of a tile's key codes to LDS, where P_K^T was, a tile before they are needed
+    // the wavefront's part of a tile's key codes to LDS, a tile before they are needed
     auto unpack = [&](int tile) {
         if (fh < nk) {
             rc_h8 zz[2];
@@ -808,7 +825,8 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll 1
     for (int tile = tile0 - 1; tile < tile1; ++tile) {
         // One wavefront of each SIMD makes the next tile and then attends to the current one, the other (late) the other way
-        // round, so that the matrix and vector work of the two overlap: the late ones meet the barrier between the two.
+        // round, so that the matrix and vector work of the two overlap: the late ones meet the barrier between the two. (256
+        // rows x 32k x 64 units: all in one order 471 us, so 353, when the rest of the kernel was simpler.)
         if (tile + 1 < tile1) make(tile + 1, sm + kBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
         if (late) __syncthreads();
         const int at = late ? tile + 1 : tile;
@@ -930,7 +948,8 @@ static_assert(kFinSmem <= 64 * 1024, "no attribute is set for it");
 
 // Block: R rows of one unit (columns of the products past R repeat the last row). z = sum_c acc_c 2^(m_c - M) over the unit's
 // pieces, the drafted tokens' weights 2^(s - M), out = (step_V P_V^T z + sum_m p_m xv_m) / l. With few rows in all, blocks
-// of four rows, whose threads also share the pieces.
+// of four rows, whose threads also share the pieces. Bound by latency, a chain of four reads of memory (8 to 10 us up to 64
+// rows x 64 units), and at 256 rows by the pieces' 42 MB.
 template <int R>
 __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, const uint16_t* __restrict__ q, int G, int n_tok,
                                                                   const uint16_t* __restrict__ xk, int64_t xk_stride,
@@ -1160,6 +1179,11 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     TreeLayout t;
     const int U = k->n_units, tiles = (max_seq + kTile - 1) / kTile;
     t.wk.M = n_tok * G;
+    // Rows of a wavefront and wavefronts side by side in rows, the rest of the eight sharing a tile's tokens. Sixteen rows until
+    // eight wavefronts have them, then 32, since making a tile's operands costs the same for any number of rows: 256 rows x 16k
+    // x 64 units 181 us, in two blocks of 128 each making them 250; 128 rows 135 us, as 32 rows a wavefront, half of them idle,
+    // 140. As few wavefronts in rows as hold them: 52 rows 112 us in four, 121 in eight; 32 rows 104 in two, 107 in four
+    // (keys not rotated: 154 and 173, 98 and 109, 76 and 79, 57 and 72).
     t.cb = t.wk.M <= 128 ? 1 : 2;
     t.rw = t.wk.M <= 32 ? 2 : (t.wk.M <= 64 ? 4 : 8);
     t.wk.rows_pb = 16 * t.cb * t.rw;
@@ -1167,7 +1191,7 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.max_seq = max_seq;
     t.wk.k_cap_tiles = (k->capacity + kTile - 1) / kTile;
     t.wk.v_cap_tiles = (v->capacity + kTile - 1) / kTile;
-    // One block for every CU (its LDS lets no second one in), as long as there are tiles for them.
+    // One block for every CU (LDS or registers let no second one in), or two, as long as there are tiles for them.
     t.wk.U = U;
     t.wk.n_blocks = (int)std::min<int64_t>(std::max(1, device_cus() * (tree_pair(t.cb, t.rw, rope) ? 2 : 1) / t.wk.nrb), (int64_t)U * (tiles ? tiles + start_cost(t.wk.M) : 0));
     const int64_t rows = t.wk.n_blocks ? ((int64_t)t.wk.n_blocks + U) * t.wk.M : 0;
@@ -1253,8 +1277,11 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     const hipStream_t st = (hipStream_t)stream;
     const DevSide K = dev_side(k), V = dev_side(v);
     const int64_t blocks = (int64_t)t.wk.nrb * t.wk.n_blocks;
+    // Rows of a finishing block: four while sixteen would leave half the CUs without one. 8 units: 32 rows x 4k 23.5 us, with
+    // sixteen 26.2; 64 rows x 128k 127 and 130. 64 units, 32 rows x 4k, where it takes sixteen: 42.5, with four 42.6.
     const int R = (int64_t)k->n_units * ((t.wk.M + 15) / 16) < device_cus() / 2 ? 4 : 16;
-    // A block takes as many groups of R rows, one after another, as it takes to have no second turn of blocks (two fit a CU).
+    // A block takes as many groups of R rows, one after another, as it takes to have no second turn of blocks (two fit a CU):
+    // 256 rows x 4k x 64 units (keys not rotated) 74.2 -> 70.3 us.
     const int64_t all_groups = (int64_t)k->n_units * ((t.wk.M + R - 1) / R), turn = 2 * (int64_t)device_cus();
     const int groups = (int)std::min<int64_t>((t.wk.M + R - 1) / R, (all_groups + turn - 1) / turn);
     const int64_t fin = (int64_t)k->n_units * ((t.wk.M + groups * R - 1) / (groups * R));
