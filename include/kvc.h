@@ -396,8 +396,9 @@ int kvc_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stri
  *              p = softmax over the visible t (q . k_t / sqrt(d)) and m (q . xk_m / sqrt(d));
  *              0 in a row that sees nothing.
  *  ws          device workspace of >= kvc_tree_attn_workspace(...) bytes, 256-byte aligned, contents ignored.
- * Softmax statistics and sums are fp32; rotated cached keys and softmax weights are rounded to fp16, like the
- * result. No atomics: results are deterministic. Async on `stream`.
+ * Softmax statistics and sums are fp32; softmax weights are rounded to fp16, like the result, and rotated cached
+ * keys to fp16 with a rest of two more bits. No atomics: results are deterministic. Async on `stream`.
+ * KVC_EUNSUPPORTED: G or n_tok out of range, a unit's stream past 2 GiB, more than 2^30 tiles of 64 tokens in all.
  */
 int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* q, int32_t G, int32_t n_tok,
                   const uint16_t* xk, int64_t xk_unit_stride, const uint16_t* xv, int64_t xv_unit_stride,
@@ -419,7 +420,7 @@ size_t kvc_tree_attn_workspace(const kvc_stream_desc* k, const kvc_stream_desc* 
  * Unit u's row rows[u][i] is encoded at position t0[u] + i, i < n[u], with the codes of kvc_encode. Being device
  * data, rows, t0 and n are not validated: n is clamped to [0, max_n], a row index to [0, n_rows - 1], and
  * positions outside [0, capacity) are left out. Streams of different units must not overlap. Every other
- * token's codes are preserved. Async on `stream`.
+ * token's codes are preserved. KVC_EUNSUPPORTED: more than 64 tokens to more than 65535 units. Async on `stream`.
  */
 int kvc_append_rows(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* xk, int64_t xk_unit_stride,
                     const uint16_t* xv, int64_t xv_unit_stride, int32_t n_rows, const int32_t* rows, const int32_t* t0,

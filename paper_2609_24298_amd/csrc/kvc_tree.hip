@@ -1202,6 +1202,11 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     return t;
 }
 
+// What either form needs: more blocks, as plain keys may have, leave more pieces.
+int64_t tree_need(const kvc_stream_desc* k, const kvc_stream_desc* v, int G, int n_tok, int max_seq) {
+    return std::max(tree_layout(k, v, G, n_tok, max_seq, false).total, tree_layout(k, v, G, n_tok, max_seq, true).total);
+}
+
 template <int CB, int RW, bool ROPE>
 int launch_tree_as(dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V, const uint16_t* q, const int32_t* seq_len, const TreeWork& wk,
                    const TreeRope& rope, float* acc, float2* ml) {
@@ -1232,7 +1237,7 @@ int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, in
     if (max_seq_len > k->capacity || max_seq_len > v->capacity)
         return set_error(KVC_ENOSPACE, "kvc_tree_attn: max_seq_len exceeds capacity");
     const int64_t kct = ((int64_t)k->capacity + kTile - 1) / kTile, vct = ((int64_t)v->capacity + kTile - 1) / kTile;
-    if ((int64_t)k->n_units * (((int64_t)max_seq_len + kTile - 1) / kTile) > INT32_MAX / 2)
+    if ((int64_t)k->n_units * (((int64_t)max_seq_len + kTile - 1) / kTile + start_cost(0)) > INT32_MAX / 2)  // counted in 32 bits
         return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: more than 2^30 tiles of 64 tokens");
     for (int u = 0; u < k->n_units; ++u)  // byte offsets inside a stream are 32 bits
         if (kct * 8 * k->r_host[u] * k->b_host[u] > INT32_MAX || vct * 8 * v->r_host[u] * v->b_host[u] > INT32_MAX)
@@ -1248,7 +1253,7 @@ using namespace kvc;
 extern "C" size_t kvc_tree_attn_workspace(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok, int32_t max_seq_len) {
     clear_error();
     if (tree_check(k, v, G, n_tok, max_seq_len)) return 0;
-    return (size_t)tree_layout(k, v, G, n_tok, max_seq_len, false).total;
+    return (size_t)tree_need(k, v, G, n_tok, max_seq_len);
 }
 
 extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* q, int32_t G, int32_t n_tok,
@@ -1270,8 +1275,8 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     if (!ws) return set_error(KVC_EINVAL, "kvc_tree_attn: null workspace");
     if (reinterpret_cast<uintptr_t>(ws) & 255) return set_error(KVC_EINVAL, "kvc_tree_attn: workspace not 256-byte aligned");
     const TreeLayout t = tree_layout(k, v, G, n_tok, max_seq_len, rope_base != 0.f);
-    if ((int64_t)ws_bytes < t.total)
-        return set_error(KVC_ENOSPACE, "kvc_tree_attn: workspace %zu < %lld bytes", ws_bytes, (long long)t.total);
+    if (const int64_t need = tree_need(k, v, G, n_tok, max_seq_len); (int64_t)ws_bytes < need)
+        return set_error(KVC_ENOSPACE, "kvc_tree_attn: workspace %zu < %lld bytes", ws_bytes, (long long)need);
     float* acc = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + t.acc);
     float2* ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(ws) + t.ml);
     const hipStream_t st = (hipStream_t)stream;

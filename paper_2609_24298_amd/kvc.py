@@ -447,7 +447,8 @@ def kvc_tree_attn(k: Side, v: Side, q, G: int, xk, xv, mask, seq_len, max_seq_le
     attends to drafted token m; seq_len: int32 (n_units,); rope_base 0: cached keys are not rotated; ws: uint8 workspace."""
     import torch
     U, half, dev = k.n_units, torch.float16, q.get_device()
-    assert q.dim() == 4 and v.n_units == U and k.codes.get_device() == dev and ws.get_device() == dev
+    assert q.dim() == 4 and v.n_units == U
+    assert k.codes.get_device() == dev and v.codes.get_device() == dev and ws.get_device() == dev
     N = q.shape[1]
     assert q.shape == (U, N, G, HEAD_DIM) and q.dtype is half and q.is_contiguous() and _is(out, half, U * N * G * HEAD_DIM, dev)
     sk, sv = _rows(xk, half, (U, N), dev), _rows(xv, half, (U, N), dev)

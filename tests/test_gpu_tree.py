@@ -89,7 +89,16 @@ def test_far_logits_stay_finite():
     q, xk, xv, words = draw(units, 4, 4, 9, scale=200.0)
     got = run_tree(units, half(q), half(xk), half(xv), words, [500], 500, BASE)
     assert torch.isfinite(got).all()
-    # the plain form's fp16 keys leave logits of this size uncertain by their rounding: only finiteness is asked
+    # the rounding of the keys leaves logits of this size uncertain: only finiteness is asked
+
+
+@pytest.mark.parametrize("base", [BASE, 0.0])
+def test_the_largest_queries_stay_finite(base):
+    units = Units([(128, 2, 64, 2), (64, 8, 128, 1)], 300, 12)
+    q, xk, xv, words = draw(units, 5, 4, 12)
+    q = (np.sign(q.astype(np.float32)) * 65504).astype(np.float16)  # vectors of the largest norm that fp16 has
+    got = run_tree(units, half(q), half(xk), half(xv), words, [300, 130], 300, base)
+    assert torch.isfinite(got).all()
 
 
 def test_empty_rows_and_unnamed_drafts():

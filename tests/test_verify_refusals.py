@@ -44,6 +44,8 @@ def test_tree_refuses_descriptors():
     assert tree(v=Desc(1, n_units=3)) == E
     assert tree(k=Desc(0, r=5)) == U and tree(k=Desc(0, b=9)) == U
     assert tree(k=Desc(0, capacity=2 ** 31 - 1, r=128, b=8), v=Desc(1, capacity=2 ** 31 - 1)) in (U, S)
+    many = [Desc(side, n_units=40, capacity=2 ** 31 - 64, r=2, b=1) for side in (0, 1)]
+    assert tree(k=many[0], v=many[1], m=2 ** 31 - 64) == U  # tiles are counted in 32 bits
     assert kvc.lib().kvc_tree_attn(None, None, None, 4, 8, None, 0, None, 0, None, None, 0, 0.0, None, None, 0, None) == E
 
 
@@ -99,3 +101,4 @@ def test_append_rows_of_nothing_and_descriptors():
     assert rows(max_n=0) == kvc.KVC_OK
     assert rows(k=Desc(1)) == E and rows(v=Desc(0)) == E and rows(v=Desc(1, n_units=1)) == E
     assert rows(k=Desc(0, n_units=0), v=Desc(1, n_units=0)) == kvc.KVC_OK
+    assert rows(k=Desc(0, n_units=65536), v=Desc(1, n_units=65536), max_n=65, m=128, sk=16384, sv=16384) == U
