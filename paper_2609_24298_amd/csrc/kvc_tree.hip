@@ -1040,23 +1040,48 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
             const bool have = 8 * mc < ((rv + 15) & ~15);
             const float* ar = acc + (slot0 * wk.M + mrow) * kD + (have ? 8 * mc : 0);
             const int64_t stride = (int64_t)wk.M * kD;
-            for (int c = mi; c < n_pieces; c += 16 * CG) Mp = fmaxf(Mp, mlr[(int64_t)c * wk.M].x);
+            auto raise = [&](float m) {  // to the maximum m: returns what weights are relative to
+                const float top = fmaxf(Mp, m), ref = top == -INFINITY ? 0.f : top, w = __builtin_amdgcn_exp2f(Mp - ref);
+                Mp = top;
+                l *= w;
 #pragma unroll
-            for (int o = 1; o < 16 * CG; o <<= 1) Mp = fmaxf(Mp, __shfl_xor(Mp, o));
-#pragma unroll 4
-            for (int c = cg; c < n_pieces; c += CG) {
-                const float2 v = mlr[(int64_t)c * wk.M];
-                const float4 a = *reinterpret_cast<const float4*>(ar + c * stride), b = *reinterpret_cast<const float4*>(ar + c * stride + 4);
-                const float w = __builtin_amdgcn_exp2f(v.x - Mp);
-                l = fmaf(w, v.y, l);
-                z[0] = fmaf(w, a.x, z[0]); z[1] = fmaf(w, a.y, z[1]); z[2] = fmaf(w, a.z, z[2]); z[3] = fmaf(w, a.w, z[3]);
-                z[4] = fmaf(w, b.x, z[4]); z[5] = fmaf(w, b.y, z[5]); z[6] = fmaf(w, b.z, z[6]); z[7] = fmaf(w, b.w, z[7]);
+                for (int e = 0; e < 8; ++e) z[e] *= w;
+                return ref;
+            };
+            constexpr int kAt = 4;  // pieces requested at once, with their maxima: no pass for the maxima first
+            for (int c0 = cg; c0 < n_pieces; c0 += kAt * CG) {
+                float2 v[kAt];
+                float4 a[kAt], b[kAt];
+#pragma unroll
+                for (int j = 0; j < kAt; ++j) {
+                    const int c = c0 + j * CG < n_pieces ? c0 + j * CG : c0;
+                    v[j] = mlr[(int64_t)c * wk.M];
+                    a[j] = *reinterpret_cast<const float4*>(ar + c * stride);
+                    b[j] = *reinterpret_cast<const float4*>(ar + c * stride + 4);
+                }
+#pragma unroll
+                for (int j = 1; j < kAt; ++j)
+                    if (c0 + j * CG >= n_pieces) v[j].x = -INFINITY;
+                const float ref = raise(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
+#pragma unroll
+                for (int j = 0; j < kAt; ++j) {
+                    const float w = __builtin_amdgcn_exp2f(v[j].x - ref);
+                    l = fmaf(w, v[j].y, l);
+                    z[0] = fmaf(w, a[j].x, z[0]); z[1] = fmaf(w, a[j].y, z[1]); z[2] = fmaf(w, a[j].z, z[2]); z[3] = fmaf(w, a[j].w, z[3]);
+                    z[4] = fmaf(w, b[j].x, z[4]); z[5] = fmaf(w, b[j].y, z[5]); z[6] = fmaf(w, b[j].z, z[6]); z[7] = fmaf(w, b[j].w, z[7]);
+                }
             }
+            if constexpr (CG > 1) {  // the row's other threads
+                float m = Mp;
 #pragma unroll
-            for (int o = 16; o < 16 * CG; o <<= 1) {
-                l += __shfl_xor(l, o);
+                for (int o = 16; o < 16 * CG; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+                raise(m);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] += __shfl_xor(z[e], o);
+                for (int o = 16; o < 16 * CG; o <<= 1) {
+                    l += __shfl_xor(l, o);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] += __shfl_xor(z[e], o);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] = have ? z[e] : 0.f;
