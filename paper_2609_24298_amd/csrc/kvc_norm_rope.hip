@@ -10,7 +10,9 @@
 // rounding to fewer bits is the one to fp16 on the way out (the unrotated and the rotated key are both
 // rounded from the fp32 norm, not one from the other).
 //
-// Bound by memory.
+// Bound by memory where there is much of it: 16384 tokens of 48 heads 68 us, 436 MB at 6.4 TB/s (a large copy reaches 5.2 to
+// 5.4), with vector instructions 89 % of the time. One token 3.2 us, 488 tokens of 80 heads 8 us: latency, and less than a
+// call's 13 us on the host.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
