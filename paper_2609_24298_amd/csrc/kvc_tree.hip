@@ -60,6 +60,9 @@ __device__ __forceinline__ rc_h2 to_half2(float x, float y) {
     return __builtin_bit_cast(rc_h2, r);
 }
 
+// x = x y + z where x stands (the compiler's own choice for a value carried round a loop costs a copy).
+__device__ __forceinline__ void fma_in_place(float& x, float y, float z) { asm("v_fma_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z)); }
+
 // Four values, times 2^11, as bf8.
 typedef short s2v __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ s2v bf8_pairs(const float (&x)[4]) {
@@ -278,6 +281,12 @@ constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading
 // units at 1/2 bit 83 -> 68, 52 rows x 16k x 64 units 79.7 and 79.9 (then 75 by sharing the projection).
 constexpr bool tree_pair(int cb, int rw, bool rope) { return !rope && cb == 1 && rw <= 4; }
 constexpr int kPairLow = 2 * kTile * kD * 4;
+// Rotated keys and up to 64 rows: eight wavefronts make the tiles and four more attend, three to a SIMD. Fewer registers each, and
+// what one waits for the others fill: 64 rows x 128k x 8 units at 1/2 bit 127 -> 110 us, 52 rows x 16k x 64 units 112 -> 98, 32 rows
+// x 4k 40.3 -> 37.6.
+constexpr bool tree_split(int cb, int rw, bool rope) { return rope && cb == 1 && rw <= 4; }
+constexpr int tree_threads(int cb, int rw, bool rope) { return kTreeThreads + (tree_split(cb, rw, rope) ? 256 : 0); }
+constexpr int tree_waves_per_simd(int cb, int rw, bool rope) { return tree_pair(cb, rw, rope) ? 4 : (tree_split(cb, rw, rope) ? 3 : 2); }
 constexpr int tree_smem(int cb, int rw, bool rope) {
     if (tree_pair(cb, rw, rope)) return kPairLow + rw * 4096;
     return kTreeLead + (cb == 2 ? kTreeWaves * cb * 2048 : 2 * kTile * kD * 2);
@@ -301,17 +310,17 @@ template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
                                            const TreeRope& rope, int u, int T, int tile0, int tile1, int rb, int64_t slot,
                                            float* __restrict__ acc_out, float2* __restrict__ ml_out) {
-    constexpr bool kPair = tree_pair(CB, RW, ROPE), kShare = ROPE && CB == 1, kKeep = kShare && RW <= 4;
-    // kShare: the two wavefronts of a token block unpack half of its key codes each, a tile ahead, and meet in LDS (64 rows x 128k
-    // 134 -> 126 us, 100 rows x 16k 140 -> 136; with 32 rows a wavefront LDS has no room). kKeep: P_K^T stays in registers
-    // (138 -> 135; more rows leave no room).
-    constexpr int kCodes = kKeep ? 0 : kTreeLead;  // where two tiles' unpacked key codes are
+    constexpr bool kPair = tree_pair(CB, RW, ROPE), kSplit = tree_split(CB, RW, ROPE);
+    constexpr bool kShare = ROPE && CB == 1;
+    // kShare: the two wavefronts of a token block unpack half of its key codes each, a tile ahead, and meet in LDS behind the
+    // buffers (64 rows x 128k 134 -> 126 us, 100 rows x 16k 140 -> 136; with 32 rows a wavefront LDS has no room).
     constexpr int kBuf = kPair ? 0 : kTreeBuf, kBufV = ROPE ? kTreeBufV : kTile * kD * 2, kBufBytes = ROPE ? kTreeBufBytes : kTile * kD * 4;
-    constexpr int TW = kTreeWaves / RW, TB = 4 / TW;  // token parts, and key blocks of one
+    constexpr int NW = kSplit ? 4 : kTreeWaves, TW = NW / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // opaque: a lane's addresses are formed again for every piece, not kept across all of them
     const int wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
-    const int rw = wv % RW, tw = wv / RW;
+    const bool maker = !kSplit || wv < kTreeWaves, attends = !kSplit || wv >= kTreeWaves;  // roles of the wavefront
+    const int aw = kSplit ? max(wv - kTreeWaves, 0) : wv, rw = aw % RW, tw = aw / RW;
     const int row0 = rb * wk.rows_pb + 16 * CB * rw;  // the wavefront's rows
     const int64_t prow = slot * wk.M;
     const int rk = uni(K.r[u]), bk = uni(K.b[u]), rv = uni(V.r[u]), bv = uni(V.b[u]);
@@ -355,7 +364,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const uint16_t* Pg = K.basis + K.basis_off[u];
     uint4 pr[kBasisItems];
     if constexpr (ROPE) {
-        basis_t_load<KVC_SIDE_K>(pr, Pg, rk, basis_item(tid));
+        if (maker) basis_t_load<KVC_SIDE_K>(pr, Pg, rk, basis_item(tid));
     } else {
 #pragma unroll
         for (int j = 0; j < kBasisItems; ++j) {
@@ -372,27 +381,30 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     rc_h8 qr[CB][4], qf[QW][CB][4];
     v8i q1 = {};
     float base[CB];  // the centre's share of a row's raw products, -(2^(b-1) - 1/2) sum_i q_i
+    if (attends)
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        const int row = row0 + 16 * cb + col;
-        const uint16_t* qp = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD;
+        for (int cb = 0; cb < CB; ++cb) {
+            const int row = row0 + 16 * cb + col;
+            const uint16_t* qp = q + ((int64_t)u * wk.M + (row < wk.M ? row : 0)) * kD;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            uint4 x;
-            if constexpr (ROPE) {
-                const uint2 a = *reinterpret_cast<const uint2*>(qp + 4 * grp + 32 * ks), b = *reinterpret_cast<const uint2*>(qp + 4 * grp + 32 * ks + 16);
-                x = uint4{a.x, a.y, b.x, b.y};
-            } else {
-                x = *reinterpret_cast<const uint4*>(qp + 8 * grp + 32 * ks);
+            for (int ks = 0; ks < 4; ++ks) {
+                uint4 x;
+                if constexpr (ROPE) {
+                    const uint2 a = *reinterpret_cast<const uint2*>(qp + 4 * grp + 32 * ks), b = *reinterpret_cast<const uint2*>(qp + 4 * grp + 32 * ks + 16);
+                    x = uint4{a.x, a.y, b.x, b.y};
+                } else {
+                    x = *reinterpret_cast<const uint4*>(qp + 8 * grp + 32 * ks);
+                }
+                if (row >= wk.M) x = uint4{0u, 0u, 0u, 0u};
+                qr[cb][ks] = __builtin_bit_cast(rc_h8, x);
             }
-            if (row >= wk.M) x = uint4{0u, 0u, 0u, 0u};
-            qr[cb][ks] = __builtin_bit_cast(rc_h8, x);
         }
+    if (maker) {
+        load_k(tile0);
+        load_v(tile0);
     }
-    load_k(tile0);
-    load_v(tile0);
     if constexpr (ROPE) {
-        basis_t_store(sm, pr, basis_item(tid));
+        if (maker) basis_t_store(sm, pr, basis_item(tid));
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
@@ -416,9 +428,10 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         const _Float16 c = (_Float16)(0.5f - (float)(1 << (bk - 1)));
         const rc_h8 cc = {c, c, c, c, c, c, c, c};
         rc_f4 a = rc_f4{0.f, 0.f, 0.f, 0.f};
+        if (maker)
 #pragma unroll
-        for (int s = 0; s < 4; ++s) a = mfma_h(*reinterpret_cast<const rc_h8*>(sm + bt_block(wv, s) + bt_lane(col, grp)), cc, a);
-        if (col == 0) *reinterpret_cast<rc_f4*>(mid + 16 * wv + 4 * grp) = a * (1.f / kRawScale);
+            for (int s = 0; s < 4; ++s) a = mfma_h(*reinterpret_cast<const rc_h8*>(sm + bt_block(wv, s) + bt_lane(col, grp)), cc, a);
+        if (maker && col == 0) *reinterpret_cast<rc_f4*>(mid + 16 * wv + 4 * grp) = a * (1.f / kRawScale);
         __syncthreads();
     } else {
         // Rows of P_K, eight features to a chunk; a row's chunks are turned by four for every sixteen rows, since a read takes
@@ -512,28 +525,19 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     const rc_h8 ones = {h1, h1, h1, h1, h1, h1, h1, h1};
     float cs[2][4], sn[2][4];  // of the lane's pairs 32 fh + 16 i + 4 grp + v at its token's position, times kRawScale
 
-    rc_h8 pk[4][4];
-    if constexpr (kKeep) {
-        const uint8_t* pt = sm + bt_lane(col, grp) + bt_block(2 * fh, 0);
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pk[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s));
-    }
     // the wavefront's part of a tile's key codes to LDS, a tile before they are needed
     auto unpack = [&](int tile) {
         if (fh < nk) {
             rc_h8 zz[2];
             tree_k_frag(kw[0], bk, xk[0], zz);
-            uint8_t* dst = sm + kCodes + ((tile - tile0) & 1) * 16384 + 8192 * fh + 1024 * kb + lane * 16;
+            uint8_t* dst = sm + kTreeLead + ((tile - tile0) & 1) * 16384 + 8192 * fh + 1024 * kb + lane * 16;
             *reinterpret_cast<rc_h8*>(dst) = zz[0];
             *reinterpret_cast<rc_h8*>(dst + 4096) = zz[1];
         }
         if (tile + 1 < tile1) load_k(tile + 1);
     };
     if constexpr (kShare) {
-        if constexpr (kKeep) __syncthreads();  // P_K^T is in registers
-        unpack(tile0);
+        if (maker) unpack(tile0);
         __syncthreads();
     }
     // keys and values of a tile to a buffer; the codes of the tile after it are requested
@@ -559,14 +563,14 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const float2 a = adv[32 * fh + 16 * i + 4 * grp + v];
-                        const float c = cs[i][v], s = sn[i][v];
-                        cs[i][v] = fmaf(c, a.x, -s * a.y);
-                        sn[i][v] = fmaf(s, a.x, c * a.y);
+                        const float sy = sn[i][v] * a.y, cy = cs[i][v] * a.y;
+                        fma_in_place(cs[i][v], a.x, -sy);
+                        fma_in_place(sn[i][v], a.x, cy);
                     }
             }
         }
         if constexpr (kShare) {
-            const uint8_t* src = sm + kCodes + ((tile - tile0) & 1) * 16384 + 1024 * kb + lane * 16;
+            const uint8_t* src = sm + kTreeLead + ((tile - tile0) & 1) * 16384 + 1024 * kb + lane * 16;
             z[0] = *reinterpret_cast<const rc_h8*>(src);
             z[1] = *reinterpret_cast<const rc_h8*>(src + 4096);
             if (nk > 1) {
@@ -613,19 +617,17 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         auto rebuild = [&](auto first) {  // matrix steps `first` and `first` + 1: eight operands in flight
             constexpr int s0 = decltype(first)::value;
             rc_h8 p[2][4];
-            if constexpr (!kKeep) {
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s0 + s));
-                __builtin_amdgcn_sched_barrier(0);
-            }
+                for (int i = 0; i < 4; ++i) p[s][i] = *reinterpret_cast<const rc_h8*>(pt + bt_block(i + (i & 2), s0 + s));
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    a[i] = mfma_h(kKeep ? pk[s0 + s][i] : p[s][i], z[s0 + s], a[i]);
-                    b[i] = mfma_h(kKeep ? pk[s0 + s][i + 2] : p[s][i + 2], z[s0 + s], b[i]);
+                    a[i] = mfma_h(p[s][i], z[s0 + s], a[i]);
+                    b[i] = mfma_h(p[s][i + 2], z[s0 + s], b[i]);
                 }
         };
         rebuild(std::integral_constant<int, 0>());
@@ -744,7 +746,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         // ---- online softmax
         constexpr int NS = TB > 1 ? TB / 2 : 1;  // halves of a tile: one or two
         const uint8_t* vr = buf + kBufV + (tb0 >> 1) * 1024 + lane * 16;
-        constexpr int AV = (kPair || kKeep) && NV > 4 ? 4 : NV;  // operands read ahead
+        constexpr int AV = kPair && NV > 4 ? 4 : NV;  // operands read ahead
         rc_h8 vf[AV];  // N-tiles past the rank make rows that are not stored
 #pragma unroll
         for (int n = 0; n < AV; ++n) vf[n] = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
@@ -821,23 +823,40 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
         }
     };
-    const bool late = wv >= kTreeWaves / 2;
+    auto buffer = [&](int tile) { return sm + kBuf + ((tile - tile0) & 1) * kBufBytes; };
+    if constexpr (kSplit) {
+        if (maker) {
 #pragma unroll 1
-    for (int tile = tile0 - 1; tile < tile1; ++tile) {
-        // One wavefront of each SIMD makes the next tile and then attends to the current one, the other (late) the other way
-        // round, so that the matrix and vector work of the two overlap: the late ones meet the barrier between the two. (256
-        // rows x 32k x 64 units: all in one order 471 us, so 353, when the rest of the kernel was simpler.)
-        if (tile + 1 < tile1) make(tile + 1, sm + kBuf + ((tile + 1 - tile0) & 1) * kBufBytes);
-        if (late) __syncthreads();
-        const int at = late ? tile + 1 : tile;
-        if (at >= tile0 && at < tile1 && row0 < wk.M) attend(at, sm + kBuf + ((at - tile0) & 1) * kBufBytes);
-        if (!late) __syncthreads();
+            for (int tile = tile0; tile <= tile1; ++tile) {
+                if (tile < tile1) make(tile, buffer(tile));
+                __syncthreads();
+            }
+        } else {
+#pragma unroll 1
+            for (int tile = tile0; tile <= tile1; ++tile) {
+                if (tile > tile0 && row0 < wk.M) attend(tile - 1, buffer(tile - 1));
+                __syncthreads();
+            }
+        }
+    } else {
+        const bool late = wv >= kTreeWaves / 2;
+#pragma unroll 1
+        for (int tile = tile0 - 1; tile < tile1; ++tile) {
+            // One wavefront of each SIMD makes the next tile and then attends to the current one, the other (late) the other way
+            // round, so that the matrix and vector work of the two overlap: the late ones meet the barrier between the two. (256
+            // rows x 32k x 64 units: all in one order 471 us, so 353, when the rest of the kernel was simpler.)
+            if (tile + 1 < tile1) make(tile + 1, buffer(tile + 1));
+            if (late) __syncthreads();
+            const int at = late ? tile + 1 : tile;
+            if (at >= tile0 && at < tile1 && row0 < wk.M) attend(at, buffer(at));
+            if (!late) __syncthreads();
+        }
     }
     if constexpr (TW == 1) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const int row = row0 + 16 * cb + col;
-            if (row >= wk.M) continue;
+            if (!attends || row >= wk.M) continue;
             if (grp == 0) ml_out[prow + row] = float2{fmaf(m[cb], qs, -kTreeShift), L[cb][0]};
 #pragma unroll
             for (int n = 0; n < NV; ++n)
@@ -847,28 +866,29 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         static_assert(CB == 1, "token parts have sixteen rows a wavefront");
         constexpr int kPitch = kD + 4;
         float* parts = reinterpret_cast<float*>(sm + kBuf);             // [TW][16 RW][kPitch]
-        float* tops = parts + kTreeWaves * 16 * kPitch;                     // [TW][16 RW]
-        float* sums = tops + kTreeWaves * 16;                               // [TW][16 RW]
-        static_assert((kTreeWaves * 16 * (kPitch + 2)) * 4 <= tree_smem(CB, RW, ROPE) - kBuf, "parts exceed the buffers");
+        float* tops = parts + NW * 16 * kPitch;                     // [TW][16 RW]
+        float* sums = tops + NW * 16;                               // [TW][16 RW]
+        static_assert((NW * 16 * (kPitch + 2)) * 4 <= tree_smem(CB, RW, ROPE) - kBuf, "parts exceed the buffers");
         __syncthreads();  // the late wavefronts have read their last tile
-        if (grp == 0) tops[16 * wv + col] = m[0];  // wavefronts are in the order (tw, rw)
+        if (attends && grp == 0) tops[16 * aw + col] = m[0];  // wavefronts are in the order (tw, rw)
         __syncthreads();
         float t = tops[16 * rw + col];
 #pragma unroll
         for (int i = 1; i < TW; ++i) t = fmaxf(t, tops[16 * (RW * i + rw) + col]);
         const float al = m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[0] - t) * qs);
-        if (grp == 0) sums[16 * wv + col] = al * L[0][0];
+        if (attends && grp == 0) sums[16 * aw + col] = al * L[0][0];
+        if (attends)
 #pragma unroll
-        for (int n = 0; n < NV; ++n)
-            if (n < nvt) *reinterpret_cast<rc_f4*>(parts + (16 * wv + col) * kPitch + 16 * n + 4 * grp) = O[n][0] * al;
+            for (int n = 0; n < NV; ++n)
+                if (n < nvt) *reinterpret_cast<rc_f4*>(parts + (16 * aw + col) * kPitch + 16 * n + 4 * grp) = O[n][0] * al;
         __syncthreads();
-        if (tw == 0 && grp == 0 && row0 + col < wk.M) {
+        if (attends && tw == 0 && grp == 0 && row0 + col < wk.M) {
             float l = sums[16 * rw + col];
 #pragma unroll
             for (int i = 1; i < TW; ++i) l += sums[16 * (RW * i + rw) + col];
             ml_out[prow + row0 + col] = float2{fmaf(t, qs, -kTreeShift), l};
         }
-        for (int e = tid; e < 16 * RW * (kD / 4); e += kTreeThreads) {
+        for (int e = tid; e < 16 * RW * (kD / 4); e += tree_threads(CB, RW, ROPE)) {
             const int r = e / (kD / 4), c4 = e % (kD / 4) * 4;
             const int row = rb * wk.rows_pb + r;
             if (c4 >= 16 * nvt || row >= wk.M) continue;
@@ -881,14 +901,16 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 }
 
 template <int CB, int RW, bool ROPE>
-__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(tree_pair(CB, RW, ROPE) ? 4 : 2, tree_pair(CB, RW, ROPE) ? 4 : 2))) void tree_partial_kernel(
+__global__ __launch_bounds__(tree_threads(CB, RW, ROPE)) __attribute__((
+    amdgpu_waves_per_eu(tree_waves_per_simd(CB, RW, ROPE), tree_waves_per_simd(CB, RW, ROPE)))) void tree_partial_kernel(
     DevSide K, DevSide V, const uint16_t* __restrict__ q, const int32_t* __restrict__ seq_len, TreeWork wk, TreeRope rope,
     float* __restrict__ acc_out, float2* __restrict__ ml_out) {
+    constexpr int kThreads = tree_threads(CB, RW, ROPE), kWaves = kThreads / 64;
     const int rb = blockIdx.x % wk.nrb, b = blockIdx.x / wk.nrb;
     const int tid = threadIdx.x, lane = tid & 63, wv = uni(tid >> 6);
     // the block's run of tiles and where it begins: a thread counts the tiles of some consecutive units
-    uint32_t* waves = reinterpret_cast<uint32_t*>(kvc_dsm);  // [8] tiles of each wavefront's units, then the first unit and tile
-    const int cu = (wk.U + kTreeThreads - 1) / kTreeThreads, u_lo = min(wk.U, tid * cu), u_hi = min(wk.U, u_lo + cu);
+    uint32_t* waves = reinterpret_cast<uint32_t*>(kvc_dsm);  // tiles of each wavefront's units, then the first unit and tile
+    const int cu = (wk.U + kThreads - 1) / kThreads, u_lo = min(wk.U, tid * cu), u_hi = min(wk.U, u_lo + cu);
     uint32_t mine = 0;
     for (int i = u_lo; i < u_hi; ++i) mine += unit_work(unit_tiles(seq_len, i, wk.max_seq), wk.M);
     uint32_t upto = mine;  // within the wavefront
@@ -899,7 +921,7 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(tr
     if (lane == 63) waves[wv] = upto;
     __syncthreads();
     uint32_t total = 0, before = upto - mine;
-    for (int i = 0; i < kTreeWaves; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
         if (i < wv) before += waves[i];
         total += waves[i];
     }
@@ -910,11 +932,11 @@ __global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(tr
         int u = u_lo;
         uint32_t at = before;
         for (uint32_t n; at + (n = unit_work(unit_tiles(seq_len, u, wk.max_seq), wk.M)) <= g; ++u) at += n;
-        waves[kTreeWaves] = u;
-        waves[kTreeWaves + 1] = g - at;
+        waves[kWaves] = u;
+        waves[kWaves + 1] = g - at;
     }
     __syncthreads();
-    int u = uni((int)waves[kTreeWaves]), x0 = uni((int)waves[kTreeWaves + 1]);  // the run begins at x0 of unit u
+    int u = uni((int)waves[kWaves]), x0 = uni((int)waves[kWaves + 1]);  // the run begins at x0 of unit u
     int left = uni((int)(g1 - g));
 #pragma unroll 1
     for (; left > 0; ++u, x0 = 0) {
@@ -1237,7 +1259,7 @@ int launch_tree_as(dim3 grid, hipStream_t st, const DevSide& K, const DevSide& V
                    const TreeRope& rope, float* acc, float2* ml) {
     const hipError_t e = hipFuncSetAttribute((const void*)tree_partial_kernel<CB, RW, ROPE>, hipFuncAttributeMaxDynamicSharedMemorySize, tree_smem(CB, RW, ROPE));
     if (e != hipSuccess) return set_error(KVC_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(kTreeThreads), tree_smem(CB, RW, ROPE), st, K, V, q, seq_len, wk, rope, acc, ml);
+    hipLaunchKernelGGL((tree_partial_kernel<CB, RW, ROPE>), grid, dim3(tree_threads(CB, RW, ROPE)), tree_smem(CB, RW, ROPE), st, K, V, q, seq_len, wk, rope, acc, ml);
     return check_launch("kvc_tree_attn");
 }
 
