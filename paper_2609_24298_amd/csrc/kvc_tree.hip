@@ -66,7 +66,7 @@ __device__ __forceinline__ void fma_in_place(float& x, float y, float z) { asm("
 // Four values, times 2^11, as bf8.
 typedef short s2v __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ s2v bf8_pairs(const float (&x)[4]) {
-    s2v r = {0, 0};
+    s2v r = __builtin_bit_cast(s2v, x[0]);  // (both halves are written: any register will do)
     r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, x[0], x[1], 1.f / kTreeLoScale, false);
     return __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, x[2], x[3], 1.f / kTreeLoScale, true);
 }
