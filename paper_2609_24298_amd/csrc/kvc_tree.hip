@@ -10,7 +10,7 @@
 // What bounds it (2 bits per dimension, 64 units of ragged lengths unless said, times of both kernels):
 //  256 rows x 32k  317 us, 675 TFLOP/s of score and value products: vector instructions 45 % of the time, matrix units 36 %, which
 //                  two wavefronts a SIMD (256 registers each) overlap only in part; the rest is waits of a step for the one before.
-//   64 rows x 128k, 8 units at 1/2 bit  127 us: making the keys (rotation, splitting), which costs the same for one row or 64.
+//   64 rows x 128k, 8 units at 1/2 bit  108 us: making the keys (rotation, splitting), which costs the same for one row or 64.
 //   52 rows x 16k, keys not rotated  75 us: the latency of a tile's steps; vector instructions 32 %, matrix units 19 %, LDS 23 %.
 //   20 rows x 300  17 us: two launches of 7 to 9 us, each a chain of four reads of memory.
 // (The bytes, at most 110 MB a call, are never the bound.)
@@ -94,8 +94,10 @@ __device__ __forceinline__ int unit_tokens(const int32_t* __restrict__ seq_len, 
 __device__ __forceinline__ int unit_tiles(const int32_t* __restrict__ seq_len, int u, int max_seq) {
     return (unit_tokens(seq_len, u, max_seq) + kTile - 1) / kTile;
 }
-// 64 units x 4k x 32 rows 48.3 -> 45.0 us, x 16k x 52 rows 114.7 -> 109.3; 8 units x 128k, which divide evenly without, 135 -> 139.
-__host__ __device__ constexpr int start_cost(int M) { return M <= 64 ? 5 : 2; }
+// 64 units x 4k x 32 rows 48.3 us without, 45.0 with, x 16k x 52 rows 114.7 and 109.3; 8 units x 128k, which divide evenly without,
+// 135 and 139. Three or seven instead of five are no better (38.4 and 37.7 against 38.0, 95.1 and 96.5 against 94.6); with 256 rows
+// x 4k 80.4 us with two, 78.6 with four.
+__host__ __device__ constexpr int start_cost(int M) { return M <= 64 ? 5 : 4; }
 __device__ __forceinline__ uint32_t unit_work(int tiles, int M) { return tiles ? (uint32_t)(tiles + start_cost(M)) : 0u; }
 // (32 bits: the host refuses more tiles)
 __device__ __forceinline__ uint32_t run_tiles(uint32_t total, int n_blocks) { return (total + (uint32_t)n_blocks - 1u) / (uint32_t)n_blocks; }
@@ -284,7 +286,7 @@ constexpr int kPairLow = 2 * kTile * kD * 4;
 // Rotated keys and up to 64 rows: eight wavefronts make the tiles and four more attend, three to a SIMD. Fewer registers each, and
 // what one waits for the others fill: 64 rows x 128k x 8 units at 1/2 bit 127 -> 110 us, 52 rows x 16k x 64 units 112 -> 98, 32 rows
 // x 4k 40.3 -> 37.6.
-constexpr bool tree_split(int cb, int rw, bool rope) { return rope && cb == 1 && rw <= 4; }
+constexpr bool tree_split(int cb, int rw, bool rope) { return rope && cb == 1 && rw == 4; }
 constexpr int tree_threads(int cb, int rw, bool rope) { return kTreeThreads + (tree_split(cb, rw, rope) ? 256 : 0); }
 constexpr int tree_waves_per_simd(int cb, int rw, bool rope) { return tree_pair(cb, rw, rope) ? 4 : (tree_split(cb, rw, rope) ? 3 : 2); }
 constexpr int tree_smem(int cb, int rw, bool rope) {
@@ -292,10 +294,10 @@ constexpr int tree_smem(int cb, int rw, bool rope) {
     return kTreeLead + (cb == 2 ? kTreeWaves * cb * 2048 : 2 * kTile * kD * 2);
 }
 
-// Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, the
-// wavefronts make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
+// Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, eight
+// wavefronts (all, or those that only make) make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
 // (K^T = P_K^T Z^T), rotates them, and unpacks the values of N-tile w, all to LDS in operand order. Wavefront (rw, tw) of RW x
-// 8 / RW then takes rows 16 CB rw .. and the tw-th part of the tile's tokens: S^T = K Q^T, the online softmax, O^T += Z_V^T P^T.
+// 8 / RW (or one of four that only attend) takes rows 16 CB rw .. and the tw-th part of the tile's tokens: S^T = K Q^T, the online softmax, O^T += Z_V^T P^T.
 // Key row m of block tb is the token whose value sits in slot (tb, m % 4) of quarter m / 4, so that the lane that computes
 // a weight is the lane whose operand needs it.
 // A rotated key is fp16 and the rest of it bf8 at 2^11 times its size, met by the queries' leading bits (e5m2 is fp16's upper byte):
@@ -863,32 +865,31 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 if (n < nvt) *reinterpret_cast<rc_f4*>(acc_out + (prow + row) * kD + 16 * n + 4 * grp) = O[n][cb];
         }
     } else {  // the token parts meet in LDS (the tiles' buffers)
-        static_assert(CB == 1, "token parts have sixteen rows a wavefront");
+        static_assert(CB == 1 && !kSplit, "token parts have sixteen rows a wavefront, of every wavefront");
         constexpr int kPitch = kD + 4;
         float* parts = reinterpret_cast<float*>(sm + kBuf);             // [TW][16 RW][kPitch]
         float* tops = parts + NW * 16 * kPitch;                     // [TW][16 RW]
         float* sums = tops + NW * 16;                               // [TW][16 RW]
         static_assert((NW * 16 * (kPitch + 2)) * 4 <= tree_smem(CB, RW, ROPE) - kBuf, "parts exceed the buffers");
         __syncthreads();  // the late wavefronts have read their last tile
-        if (attends && grp == 0) tops[16 * aw + col] = m[0];  // wavefronts are in the order (tw, rw)
+        if (grp == 0) tops[16 * wv + col] = m[0];  // wavefronts are in the order (tw, rw)
         __syncthreads();
         float t = tops[16 * rw + col];
 #pragma unroll
         for (int i = 1; i < TW; ++i) t = fmaxf(t, tops[16 * (RW * i + rw) + col]);
         const float al = m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[0] - t) * qs);
-        if (attends && grp == 0) sums[16 * aw + col] = al * L[0][0];
-        if (attends)
+        if (grp == 0) sums[16 * wv + col] = al * L[0][0];
 #pragma unroll
-            for (int n = 0; n < NV; ++n)
-                if (n < nvt) *reinterpret_cast<rc_f4*>(parts + (16 * aw + col) * kPitch + 16 * n + 4 * grp) = O[n][0] * al;
+        for (int n = 0; n < NV; ++n)
+            if (n < nvt) *reinterpret_cast<rc_f4*>(parts + (16 * wv + col) * kPitch + 16 * n + 4 * grp) = O[n][0] * al;
         __syncthreads();
-        if (attends && tw == 0 && grp == 0 && row0 + col < wk.M) {
+        if (tw == 0 && grp == 0 && row0 + col < wk.M) {
             float l = sums[16 * rw + col];
 #pragma unroll
             for (int i = 1; i < TW; ++i) l += sums[16 * (RW * i + rw) + col];
             ml_out[prow + row0 + col] = float2{fmaf(t, qs, -kTreeShift), l};
         }
-        for (int e = tid; e < 16 * RW * (kD / 4); e += tree_threads(CB, RW, ROPE)) {
+        for (int e = tid; e < 16 * RW * (kD / 4); e += kTreeThreads) {
             const int r = e / (kD / 4), c4 = e % (kD / 4) * 4;
             const int row = rb * wk.rows_pb + r;
             if (c4 >= 16 * nvt || row >= wk.M) continue;
@@ -1229,10 +1230,10 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     // Rows of a wavefront and wavefronts side by side in rows, the rest of the eight sharing a tile's tokens. Sixteen rows until
     // eight wavefronts have them, then 32, since making a tile's operands costs the same for any number of rows: 256 rows x 16k
     // x 64 units 181 us, in two blocks of 128 each making them 250; 128 rows 135 us, as 32 rows a wavefront, half of them idle,
-    // 140. As few wavefronts in rows as hold them: 52 rows 112 us in four, 121 in eight; 32 rows 104 in two, 107 in four
-    // (keys not rotated: 154 and 173, 98 and 109, 76 and 79, 57 and 72).
+    // 140 (keys not rotated: 154 and 173, 98 and 109). As few wavefronts in rows as hold them: 52 rows 98 us in four (that only
+    // attend), 118 in eight; keys not rotated 76 and 79, and 32 rows 57 in two and 72 in four (rotated 94 and 92).
     t.cb = t.wk.M <= 128 ? 1 : 2;
-    t.rw = t.wk.M <= 32 ? 2 : (t.wk.M <= 64 ? 4 : 8);
+    t.rw = t.wk.M > 64 ? 8 : (t.wk.M > 32 || rope ? 4 : 2);
     t.wk.rows_pb = 16 * t.cb * t.rw;
     t.wk.nrb = (t.wk.M + t.wk.rows_pb - 1) / t.wk.rows_pb;
     t.wk.max_seq = max_seq;
@@ -1268,8 +1269,9 @@ int launch_tree(const TreeLayout& t, dim3 grid, hipStream_t st, const DevSide& K
                 const TreeRope& rope, float* acc, float2* ml) {
     if (t.cb == 2) return launch_tree_as<2, 8, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
     if (t.rw == 8) return launch_tree_as<1, 8, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
-    if (t.rw == 4) return launch_tree_as<1, 4, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
-    return launch_tree_as<1, 2, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
+    if constexpr (!ROPE)
+        if (t.rw == 2) return launch_tree_as<1, 2, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
+    return launch_tree_as<1, 4, ROPE>(grid, st, K, V, q, seq_len, t.wk, rope, acc, ml);
 }
 
 int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok, int32_t max_seq_len) {
