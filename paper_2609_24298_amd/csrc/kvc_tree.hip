@@ -283,12 +283,13 @@ constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading
 // units at 1/2 bit 83 -> 68, 52 rows x 16k x 64 units 79.7 and 79.9 (then 75 by sharing the projection).
 constexpr bool tree_pair(int cb, int rw, bool rope) { return !rope && cb == 1 && rw <= 4; }
 constexpr int kPairLow = 2 * kTile * kD * 4;
-// Rotated keys and up to 64 rows: eight wavefronts make the tiles and four more attend, three to a SIMD. Fewer registers each, and
-// what one waits for the others fill: 64 rows x 128k x 8 units at 1/2 bit 127 -> 110 us, 52 rows x 16k x 64 units 112 -> 98, 32 rows
-// x 4k 40.3 -> 37.6.
-constexpr bool tree_split(int cb, int rw, bool rope) { return rope && cb == 1 && rw == 4; }
-constexpr int tree_threads(int cb, int rw, bool rope) { return kTreeThreads + (tree_split(cb, rw, rope) ? 256 : 0); }
-constexpr int tree_waves_per_simd(int cb, int rw, bool rope) { return tree_pair(cb, rw, rope) ? 4 : (tree_split(cb, rw, rope) ? 3 : 2); }
+// Rotated keys and up to 64 (128) rows: eight wavefronts make the tiles and four (eight) more attend, three (four) to a SIMD. Fewer
+// registers each, and what one waits for the others fill. Against eight that do both, 64 units: 32 rows x 4k 40.3 -> 36.6 us, 52
+// rows x 16k 112 -> 98, 100 rows x 16k 136 -> 122, x 4k 55.2 and 55.3; 8 units, 64 rows x 128k at 1/2 bit 127 -> 108. (32
+// rows a wavefront need more than 168 registers.)
+constexpr bool tree_split(int cb, int rw, bool rope) { return rope && cb == 1 && rw >= 4; }
+constexpr int tree_threads(int cb, int rw, bool rope) { return kTreeThreads + (tree_split(cb, rw, rope) ? 64 * rw : 0); }
+constexpr int tree_waves_per_simd(int cb, int rw, bool rope) { return tree_pair(cb, rw, rope) ? 4 : (tree_split(cb, rw, rope) ? tree_threads(cb, rw, rope) / 256 : 2); }
 constexpr int tree_smem(int cb, int rw, bool rope) {
     if (tree_pair(cb, rw, rope)) return kPairLow + rw * 4096;
     return kTreeLead + (cb == 2 ? kTreeWaves * cb * 2048 : 2 * kTile * kD * 2);
@@ -317,7 +318,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     // kShare: the two wavefronts of a token block unpack half of its key codes each, a tile ahead, and meet in LDS behind the
     // buffers (64 rows x 128k 134 -> 126 us, 100 rows x 16k 140 -> 136; with 32 rows a wavefront LDS has no room).
     constexpr int kBuf = kPair ? 0 : kTreeBuf, kBufV = ROPE ? kTreeBufV : kTile * kD * 2, kBufBytes = ROPE ? kTreeBufBytes : kTile * kD * 4;
-    constexpr int NW = kSplit ? 4 : kTreeWaves, TW = NW / RW, TB = 4 / TW;  // token parts, and key blocks of one
+    constexpr int NW = kSplit ? RW : kTreeWaves, TW = NW / RW, TB = 4 / TW;  // token parts, and key blocks of one
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // opaque: a lane's addresses are formed again for every piece, not kept across all of them
     const int wv = uni(tid >> 6), lane = tid & 63, col = lane & 15, grp = lane >> 4;
@@ -676,13 +677,15 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             constexpr int kAhead = 4;
             const uint8_t* kr = buf + (64 * grp + 16 * tb0 + col) * 16;
             auto key = [&](int i) { return *reinterpret_cast<const rc_h8*>(kr + 4096 * (i / TB) + 256 * (i % TB)); };
-            v4i l0[TB], l1[TB];
+            constexpr int kLo = kSplit && TB > 2 ? 2 : TB;  // low parts read ahead
+            v4i l0[kLo], l1[kLo];
             rc_h8 kf[kAhead];
+            auto low_part = [&](int t) {
+                l0[t % kLo] = *reinterpret_cast<const v4i*>(kr + kBufLo + 256 * t);
+                l1[t % kLo] = *reinterpret_cast<const v4i*>(kr + kBufLo + 4096 + 256 * t);
+            };
 #pragma unroll
-            for (int t = 0; t < TB; ++t) {
-                l0[t] = *reinterpret_cast<const v4i*>(kr + kBufLo + 256 * t);
-                l1[t] = *reinterpret_cast<const v4i*>(kr + kBufLo + 4096 + 256 * t);
-            }
+            for (int t = 0; t < kLo; ++t) low_part(t);
             v8i q8[CB];
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
@@ -696,9 +699,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < TB; ++t) {
-                const v8i lo = {l0[t][0], l0[t][1], l0[t][2], l0[t][3], l1[t][0], l1[t][1], l1[t][2], l1[t][3]};
+                const v4i a = l0[t % kLo], b = l1[t % kLo];
+                const v8i lo = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_lo(lo, q8[cb], rc_f4{0.f, 0.f, 0.f, 0.f});
+                if (t + kLo < TB) low_part(t + kLo);
 #pragma unroll
                 for (int i = kAhead * t / TB; i < kAhead * (t + 1) / TB; ++i) kf[i] = key(i);
                 __builtin_amdgcn_sched_barrier(0);
@@ -748,10 +753,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         // ---- online softmax
         constexpr int NS = TB > 1 ? TB / 2 : 1;  // halves of a tile: one or two
         const uint8_t* vr = buf + kBufV + (tb0 >> 1) * 1024 + lane * 16;
-        constexpr int AV = kPair && NV > 4 ? 4 : NV;  // operands read ahead
+        constexpr int AV = tree_waves_per_simd(CB, RW, ROPE) == 4 && NV > 4 ? 4 : NV;  // operands read ahead
+        auto value = [&](int k) { return *reinterpret_cast<const rc_h8*>(vr + k / NV * 1024 + k % NV * 2048); };  // of the first half, then of the second
         rc_h8 vf[AV];  // N-tiles past the rank make rows that are not stored
 #pragma unroll
-        for (int n = 0; n < AV; ++n) vf[n] = *reinterpret_cast<const rc_h8*>(vr + n * 2048);
+        for (int n = 0; n < AV; ++n) vf[n] = value(n);
         float top[CB];
         bool raise = false;
 #pragma unroll
@@ -799,7 +805,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             for (int n = 0; n < NV; ++n) {
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n % AV], P[cb], O[n][cb]);
-                if (n + AV < NV) vf[n % AV] = *reinterpret_cast<const rc_h8*>(vr + (n + AV) * 2048);
+                if (n + AV < NV) vf[n % AV] = value(n + AV);
             }
         } else {
             float w1[CB][8];
@@ -807,8 +813,8 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int n = 0; n < NV; ++n) {
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
-                vf[n] = *reinterpret_cast<const rc_h8*>(vr + 1024 + n * 2048);
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n % AV], P[cb], O[n][cb]);
+                vf[n % AV] = value(n + AV);
 #pragma unroll
                 for (int i = 8 * CB * n / NV; i < 8 * CB * (n + 1) / NV; ++i) w1[i >> 3][i & 7] = weight(1, i >> 3, i & 7);
                 __builtin_amdgcn_sched_barrier(0);
@@ -820,9 +826,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) L[cb] = mfma_h(ones, P[cb], L[cb]);
 #pragma unroll
-            for (int n = 0; n < NV; ++n)
+            for (int n = 0; n < NV; ++n) {
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[n], P[cb], O[n][cb]);
+                for (int cb = 0; cb < CB; ++cb) O[n][cb] = mfma_h(vf[(NV + n) % AV], P[cb], O[n][cb]);
+                if (n + AV < NV) vf[(NV + n) % AV] = value(NV + n + AV);
+            }
         }
     };
     auto buffer = [&](int tile) { return sm + kBuf + ((tile - tile0) & 1) * kBufBytes; };
@@ -1229,7 +1237,7 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.M = n_tok * G;
     // Rows of a wavefront and wavefronts side by side in rows, the rest of the eight sharing a tile's tokens. Sixteen rows until
     // eight wavefronts have them, then 32, since making a tile's operands costs the same for any number of rows: 256 rows x 16k
-    // x 64 units 181 us, in two blocks of 128 each making them 250; 128 rows 135 us, as 32 rows a wavefront, half of them idle,
+    // x 64 units 181 us, in two blocks of 128 each making them 250; 128 rows 129 us, as 32 rows a wavefront, half of them idle,
     // 140 (keys not rotated: 154 and 173, 98 and 109). As few wavefronts in rows as hold them: 52 rows 98 us in four (that only
     // attend), 118 in eight; keys not rotated 76 and 79, and 32 rows 57 in two and 72 in four (rotated 94 and 92).
     t.cb = t.wk.M <= 128 ? 1 : 2;
