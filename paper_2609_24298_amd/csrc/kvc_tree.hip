@@ -1237,9 +1237,9 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.M = n_tok * G;
     // Rows of a wavefront and wavefronts side by side in rows, the rest of the eight sharing a tile's tokens. Sixteen rows until
     // eight wavefronts have them, then 32, since making a tile's operands costs the same for any number of rows: 256 rows x 16k
-    // x 64 units 181 us, in two blocks of 128 each making them 250; 128 rows 129 us, as 32 rows a wavefront, half of them idle,
-    // 140 (keys not rotated: 154 and 173, 98 and 109). As few wavefronts in rows as hold them: 52 rows 98 us in four (that only
-    // attend), 118 in eight; keys not rotated 76 and 79, and 32 rows 57 in two and 72 in four (rotated 94 and 92).
+    // x 64 units 178 us, in two blocks of 128 each making them 217; 128 rows 124 us, as 32 rows a wavefront, half of them idle,
+    // 138 (keys not rotated: 151 and 170, 96 and 108). As few wavefronts in rows as hold them: 52 rows 95 us in four (that only
+    // attend), 100 in eight; keys not rotated 75 and 78, and 32 rows 57 in two and 72 in four (rotated 94 and 92).
     t.cb = t.wk.M <= 128 ? 1 : 2;
     t.rw = t.wk.M > 64 ? 8 : (t.wk.M > 32 || rope ? 4 : 2);
     t.wk.rows_pb = 16 * t.cb * t.rw;
