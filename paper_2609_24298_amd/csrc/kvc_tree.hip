@@ -8,11 +8,12 @@
 //  tree_finish_kernel   per sixteen (or four) rows: merges the pieces, applies P_V, adds the drafted tokens.
 //
 // What bounds it (2 bits per dimension, 64 units of ragged lengths unless said, times of both kernels):
-//  256 rows x 32k  317 us, 675 TFLOP/s of score and value products: vector instructions 45 % of the time, matrix units 36 %, which
+//  256 rows x 32k  310 us, 690 TFLOP/s of score and value products: vector instructions 44 % of the time, matrix units 37 %, which
 //                  two wavefronts a SIMD (256 registers each) overlap only in part; the rest is waits of a step for the one before.
-//   64 rows x 128k, 8 units at 1/2 bit  108 us: making the keys (rotation, splitting), which costs the same for one row or 64.
+//   64 rows x 128k, 8 units at 1/2 bit  108 us: the wavefronts that make the keys (rotation, splitting), the same for one row or
+//                  64; vector instructions 44 %, LDS 45 %, matrix units 23 %.
 //   52 rows x 16k, keys not rotated  75 us: the latency of a tile's steps; vector instructions 32 %, matrix units 19 %, LDS 23 %.
-//   20 rows x 300  17 us: two launches of 7 to 9 us, each a chain of four reads of memory.
+//   20 rows x 300  17 us: two launches of 7 to 10 us, each a chain of four reads of memory.
 // (The bytes, at most 110 MB a call, are never the bound.)
 #define KVC_DECODE_PARTIALS_UNIT
 #include "kvc_decode.hip"
