@@ -827,7 +827,7 @@ extern "C" int kvc_append_rows(const kvc_stream_desc* k, const kvc_stream_desc* 
                            a, k->n_units, most);
     } else {
         if (k->n_units > 65535) return set_error(KVC_EUNSUPPORTED, "kvc_append_rows: more than 65535 units and more than %d tokens", kRowsFewMax);
-        const int n_tiles = (max_n + 2 * kTile - 2) / kTile;  // of the longest run, wherever in a tile it begins
+        const int n_tiles = (int)(((int64_t)max_n + 2 * kTile - 2) / kTile);  // of the longest run, wherever in a tile it begins
         const int tpb = encode_tpb(2ll * k->n_units, n_tiles);
         hipLaunchKernelGGL(encode_rows_kernel, dim3((n_tiles + tpb - 1) / tpb, k->n_units, 2), dim3(kEncMmaThreads), kEncSmem,
                            (hipStream_t)stream, dev_side(k), dev_side(v), a, tpb);

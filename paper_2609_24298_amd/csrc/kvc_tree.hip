@@ -1294,6 +1294,7 @@ int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, in
     if (max_seq_len < 0) return set_error(KVC_EINVAL, "kvc_tree_attn: negative max_seq_len");
     if (max_seq_len > k->capacity || max_seq_len > v->capacity)
         return set_error(KVC_ENOSPACE, "kvc_tree_attn: max_seq_len exceeds capacity");
+    if (max_seq_len > INT32_MAX - kTile + 1) return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: max_seq_len past 2^31 - 64");
     const int64_t kct = ((int64_t)k->capacity + kTile - 1) / kTile, vct = ((int64_t)v->capacity + kTile - 1) / kTile;
     if ((int64_t)k->n_units * (((int64_t)max_seq_len + kTile - 1) / kTile + start_cost(0)) > INT32_MAX / 2)  // counted in 32 bits
         return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: more than 2^30 tiles of 64 tokens");

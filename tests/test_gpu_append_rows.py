@@ -75,6 +75,15 @@ def test_more_units_than_the_device_has_units_of_work(max_n, scale):
     run(units, xk, xv, pick, t0, n)
 
 
+@pytest.mark.parametrize("U,max_n", [(3, 2), (3, 20), (260, 2), (260, 20), (260, 90)])
+def test_unaligned_bases(U, max_n):
+    units = Units([(RANKS[i % 10], 1 + i % 8, RANKS[(i + 3) % 10], 1 + (i // 8) % 8) for i in range(U)], 120, 30, lead=5)
+    rng = np.random.default_rng(30)
+    xk, xv = tokens(U, max_n, 31), tokens(U, max_n, 32)
+    pick = rng.integers(0, max_n, (U, max_n))
+    run(units, xk, xv, pick, rng.integers(0, 120, U), rng.integers(0, max_n + 1, U))
+
+
 @pytest.mark.parametrize("max_n", [5, 70])
 def test_rows_repeated_and_all_of_them(max_n):
     units = Units([(84, 3, 64, 2), (128, 2, 126, 1), (18, 7, 30, 8)], 200, 5)

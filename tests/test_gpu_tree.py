@@ -71,6 +71,39 @@ def test_sizes(U, N, G, T):
     log(f"[tree U={U} N={N} G={G} T={T}] at most {worst:.2f} of the bound")
 
 
+@pytest.mark.parametrize("base", [BASE, 0.0])
+@pytest.mark.parametrize("N,G", [(3, 4), (13, 4), (24, 4), (40, 4)])
+def test_unaligned_bases(N, G, base):
+    units = Units([(84, 3, 66, 5), (128, 2, 128, 2), (18, 8, 30, 1)], 200, 15, lead=3)
+    q, xk, xv, words = draw(units, N, G, 15)
+    lens = np.array([200, 77, 64])
+    check(units, run_tree(units, half(q), half(xk), half(xv), words, lens, 200, base), q, xk, xv, words, lens, base)
+
+
+@pytest.mark.parametrize("U,N,G,T", [(3, 64, 16, 700), (2, 17, 5, 3001), (2, 3, 2, 40000), (1, 1, 4, 130001), (3, 32, 4, 5000)])
+def test_sizes_of_plain_keys(U, N, G, T):
+    units = Units([((128, 2, 128, 2), (84, 3, 64, 4), (64, 1, 30, 1))[u] for u in range(U)], T, U + N)
+    q, xk, xv, words = draw(units, N, G, T)
+    lens = np.array([T, T // 3, 64][:U])
+    check(units, run_tree(units, half(q), half(xk), half(xv), words, lens, T, 0.0), q, xk, xv, words, lens, 0.0)
+
+
+@pytest.fixture(scope="module")
+def many_units():
+    return Units([(18, 2, 14, 2)] * 2100, 200, 16)
+
+
+@pytest.mark.parametrize("base", [BASE, 0.0])
+@pytest.mark.parametrize("N,G", [(2, 2), (10, 4), (20, 4)])
+def test_more_units_than_threads(many_units, N, G, base):
+    # a thread of a block counts the tiles of several units; lengths from none to a few tiles
+    units, U = many_units, 2100
+    q, xk, xv, words = draw(units, N, G, 16)
+    lens = np.random.default_rng(16).integers(0, 201, U)
+    got = run_tree(units, half(q), half(xk), half(xv), words, lens, 200, base)
+    check(units, got, q, xk, xv, words, lens, base, which=list(range(0, U, 97)) + [U - 1])
+
+
 def test_sharp_and_flat_attention():
     # one key far above all others, early or late in the context, and queries near zero
     units = Units([(128, 4, 128, 4)] * 3, 2000, 8)

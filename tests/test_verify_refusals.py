@@ -46,6 +46,8 @@ def test_tree_refuses_descriptors():
     assert tree(k=Desc(0, capacity=2 ** 31 - 1, r=128, b=8), v=Desc(1, capacity=2 ** 31 - 1)) in (U, S)
     many = [Desc(side, n_units=40, capacity=2 ** 31 - 64, r=2, b=1) for side in (0, 1)]
     assert tree(k=many[0], v=many[1], m=2 ** 31 - 64) == U  # tiles are counted in 32 bits
+    one = [Desc(side, n_units=1, capacity=2 ** 31 - 1, r=2, b=1) for side in (0, 1)]
+    assert tree(k=one[0], v=one[1], m=2 ** 31 - 1) == U
     assert kvc.lib().kvc_tree_attn(None, None, None, 4, 8, None, 0, None, 0, None, None, 0, 0.0, None, None, 0, None) == E
 
 

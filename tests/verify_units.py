@@ -22,7 +22,7 @@ def half(a):
 class Units:
     """Units of both sides with given (r_K, b_K, r_V, b_V), random bases, and codes of coordinates of about unit variance."""
 
-    def __init__(self, rows, capacity, seed, device="cuda"):
+    def __init__(self, rows, capacity, seed, device="cuda", lead=0):
         self.rows, self.capacity = rows, capacity
         rng = np.random.default_rng(seed)
         self.P, self.delta, self.codes, self.sides = ([], []), ([], []), ([], []), []
@@ -34,8 +34,9 @@ class Units:
                 self.delta[side].append(np.float32(rng.uniform(0.7, 1.3) * 2.2 / 2 ** (b - 1)))
                 y = rng.standard_normal((capacity, r)) * 2 ** (b - 1) / 2.2
                 self.codes[side].append(np.clip(np.floor(y) + 2 ** (b - 1), 0, 2 ** b - 1).astype(np.uint8))
-            flat = np.concatenate([p.reshape(-1) for p in self.P[side]])
-            offs = np.concatenate([[0], np.cumsum([p.size for p in self.P[side]])[:-1]]).astype(np.int64)
+            gap = np.full(lead, 0x7E00, np.uint16)  # elements before each basis (NaN), so that none need be aligned
+            flat = np.concatenate([x for p in self.P[side] for x in (gap, p.reshape(-1))])
+            offs = np.concatenate([[0], np.cumsum([p.size + lead for p in self.P[side]])[:-1]]).astype(np.int64) + lead
             S = kvc.Side(side, rs, bs, np.array(self.delta[side], np.float32), flat, offs, capacity, device)
             arena = np.zeros(S.codes.numel(), np.uint8)
             for u, (r, b) in enumerate(zip(rs, bs)):
