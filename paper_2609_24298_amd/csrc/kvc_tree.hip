@@ -296,10 +296,11 @@ constexpr int tree_smem(int cb, int rw, bool rope) {
     return kTreeLead + (cb == 2 ? kTreeWaves * cb * 2048 : 2 * kTile * kD * 2);
 }
 
-// Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, eight
-// wavefronts (all, or those that only make) make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
-// (K^T = P_K^T Z^T), rotates them, and unpacks the values of N-tile w, all to LDS in operand order. Wavefront (rw, tw) of RW x
-// 8 / RW (or one of four that only attend) takes rows 16 CB rw .. and the tw-th part of the tile's tokens: S^T = K Q^T, the online softmax, O^T += Z_V^T P^T.
+// Block: rows [rows_pb rb, ..) over one run of 64-token tiles, unit by unit. While tile t is attended, eight wavefronts (all, or
+// those that only make) make tile t + 1: wavefront w rebuilds the keys of token block w / 2, feature pairs of half w % 2
+// (K^T = P_K^T Z^T), rotates them, and unpacks the values of N-tile w, all to LDS in operand order. Wavefront (rw, tw) of RW x 8 / RW
+// (or of RW that only attend) takes rows 16 CB rw .. and the tw-th part of the tile's tokens: S^T = K Q^T, the online softmax,
+// O^T += Z_V^T P^T.
 // Key row m of block tb is the token whose value sits in slot (tb, m % 4) of quarter m / 4, so that the lane that computes
 // a weight is the lane whose operand needs it.
 // A rotated key is fp16 and the rest of it bf8 at 2^11 times its size, met by the queries' leading bits (e5m2 is fp16's upper byte):
