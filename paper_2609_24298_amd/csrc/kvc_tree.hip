@@ -32,7 +32,6 @@ constexpr float kTreeLazy = 5.f;    // the running maximum is raised when a tile
 constexpr int kTreeResync = 32;
 
 constexpr float kRawScale = 16777216.f;  // 2^24: a raw code in an fp16 operand is this times too small
-constexpr float kPlainScale = 0.0625f;   // of projected queries: one of the longest fp16 vector stays in range
 constexpr float kTreeLoScale = 2048.f;  // of the low part of a key
 constexpr int kTreeLoExp = 127 - 11;    // its scale as a matrix operand's exponent
 
@@ -307,7 +306,8 @@ constexpr int tree_smem(int cb, int rw, bool rope) {
 // logits keep about 14 bits of the key for a quarter more matrix work, where fp16 alone would put an error of 2^-12 of
 // each coordinate into the weights.
 // Keys that are not rotated are not rebuilt: q . k = (P_K q) . z up to the step, so a piece begins by projecting its queries (kept
-// as the sum of two fp16, 2^-22 off), a wavefront makes tile t + 1 by unpacking half of a token block's codes, and the
+// as the sum of two fp16, 2^-22 off; a query is taken at a scale of its own, its largest element in [1, 2), since the second
+// fp16 of a small one would be below that type's range: queries of 2^-13 lost up to 2^-8 of a logit otherwise), a wavefront makes tile t + 1 by unpacking half of a token block's codes, and the
 // products are of codes and projections. Twice the matrix steps for the scores, but the making is a quarter: 52 rows x 16k
 // x 64 units 115 us rebuilt, 78 so; 256 rows x 32k 335 and 274.
 // NV: N-tiles of values, so that ranks up to 64 and 96 do no products for the rest.
@@ -386,6 +386,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     rc_h8 qr[CB][4], qf[QW][CB][4];
     v8i q1 = {};
     float base[CB];  // the centre's share of a row's raw products, -(2^(b-1) - 1/2) sum_i q_i
+    float qexp[CB];  // plain keys: the power of two that the row's projection is divided by
     if (attends)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
@@ -449,6 +450,20 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             *reinterpret_cast<uint4*>(chunk(e >> 4, e & 15)) = pr[j];
         }
         __syncthreads();
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {  // of the row's largest element, its four lanes together
+            typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+            us2 most = {0, 0};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, __builtin_bit_cast(v4u, qr[cb][ks])[d] & 0x7fff7fffu));
+            int x = max((int)most[0], (int)most[1]);
+            x = max(x, __shfl_xor(x, 16));
+            x = max(x, __shfl_xor(x, 32));
+            qexp[cb] = x ? __uint_as_float(__float_as_uint(h2f((uint16_t)x)) & 0x7f800000u) : 1.f;
+        }
         // matrix step ks of the scores: coordinates 64 (ks / 2) + 16 grp + 4 (ks % 2) + v, and 8 further
         auto project = [&](int ks, int cb, rc_h8& hi, rc_h8& lo) {
             rc_f4 d[2];
@@ -459,9 +474,10 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
                 for (int fs = 0; fs < 4; ++fs) d[h] = mfma_h(*reinterpret_cast<const rc_h8*>(chunk(i, 4 * fs + grp)), qr[cb][fs], d[h]);
             }
+            const float down = __uint_as_float(0x7f000000u - __float_as_uint(qexp[cb]));  // 1 / qexp
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float x = d[e & 1][e >> 1] * kPlainScale;
+                const float x = d[e & 1][e >> 1] * down;
                 hi[e] = (_Float16)x;
                 lo[e] = (_Float16)(x - (float)hi[e]);
             }
@@ -507,9 +523,11 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             base[cb] = sum[0] * (1.f / kRawScale);
         }
     }
-    // step_K log2(e) / sqrt(128), and what scales a raw product
-    const float qs = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f * (ROPE ? 1.f : kRawScale / kPlainScale);
-    const float lazy = kTreeLazy / qs;
+    // step_K log2(e) / sqrt(128), and what scales a raw product of the row
+    const float unit = K.delta[u] * 1.4426950408889634f * 0.08838834764831845f;
+    float qs[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) qs[cb] = ROPE ? unit : unit * kRawScale * qexp[cb];
     float m[CB];  // running maxima of the raw products
     rc_f4 O[NV][CB], L[CB];
 #pragma unroll
@@ -769,7 +787,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             for (int t = 0; t < TB; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) top[cb] = fmaxf(top[cb], S[t][cb][v]);
-            raise = raise || top[cb] > m[cb] + lazy;
+            raise = raise || (top[cb] - m[cb]) * qs[cb] > kTreeLazy;
         }
         if (__any(raise)) {
 #pragma unroll
@@ -777,7 +795,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 float t = fmaxf(top[cb], __shfl_xor(top[cb], 16));
                 t = fmaxf(t, __shfl_xor(t, 32));
                 if (t > m[cb]) {
-                    const float al = __builtin_amdgcn_exp2f((m[cb] - t) * qs);
+                    const float al = __builtin_amdgcn_exp2f((m[cb] - t) * qs[cb]);
                     m[cb] = t;
                     L[cb] *= al;
 #pragma unroll
@@ -789,8 +807,8 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         float off[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)  // a row that has seen no token yet (a part of a short last tile) has every weight 0
-            off[cb] = TW > 1 && m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs, kTreeShift);
-        auto weight = [&](int s, int cb, int e) { return __builtin_amdgcn_exp2f(fmaf(S[TB > 1 ? 2 * s + (e >> 2) : 0][cb][e & 3], qs, off[cb])); };
+            off[cb] = TW > 1 && m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs[cb], kTreeShift);
+        auto weight = [&](int s, int cb, int e) { return __builtin_amdgcn_exp2f(fmaf(S[TB > 1 ? 2 * s + (e >> 2) : 0][cb][e & 3], qs[cb], off[cb])); };
         rc_h8 P[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
@@ -869,7 +887,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         for (int cb = 0; cb < CB; ++cb) {
             const int row = row0 + 16 * cb + col;
             if (!attends || row >= wk.M) continue;
-            if (grp == 0) ml_out[prow + row] = float2{fmaf(m[cb], qs, -kTreeShift), L[cb][0]};
+            if (grp == 0) ml_out[prow + row] = float2{fmaf(m[cb], qs[cb], -kTreeShift), L[cb][0]};
 #pragma unroll
             for (int n = 0; n < NV; ++n)
                 if (n < nvt) *reinterpret_cast<rc_f4*>(acc_out + (prow + row) * kD + 16 * n + 4 * grp) = O[n][cb];
@@ -887,7 +905,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
         float t = tops[16 * rw + col];
 #pragma unroll
         for (int i = 1; i < TW; ++i) t = fmaxf(t, tops[16 * (RW * i + rw) + col]);
-        const float al = m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[0] - t) * qs);
+        const float al = m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m[0] - t) * qs[0]);
         if (grp == 0) sums[16 * wv + col] = al * L[0][0];
 #pragma unroll
         for (int n = 0; n < NV; ++n)
@@ -897,7 +915,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             float l = sums[16 * rw + col];
 #pragma unroll
             for (int i = 1; i < TW; ++i) l += sums[16 * (RW * i + rw) + col];
-            ml_out[prow + row0 + col] = float2{fmaf(t, qs, -kTreeShift), l};
+            ml_out[prow + row0 + col] = float2{fmaf(t, qs[0], -kTreeShift), l};
         }
         for (int e = tid; e < 16 * RW * (kD / 4); e += kTreeThreads) {
             const int r = e / (kD / 4), c4 = e % (kD / 4) * 4;

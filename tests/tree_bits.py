@@ -35,13 +35,13 @@ def lead(q):
     return (q.view(np.uint16) & np.uint16(0xFF00)).view(np.float16).astype(np.float64)
 
 
-def large_queries(units, u, M, base, rng):
-    """M queries whose logits over the unit's keys are small differences: of elements about SIZE, fp16."""
+def large_queries(units, u, M, base, rng, size=SIZE):
+    """M queries whose logits over the unit's keys are small differences: of elements about `size`, fp16."""
     k = units.keys(u, TOKENS, base)
     _, _, vt = np.linalg.svd(k, full_matrices=True)
     free = vt[TOKENS:]
     q = rng.standard_normal((M, 128 - TOKENS)) @ free
-    q *= SIZE / np.sqrt((q * q).mean(axis=1, keepdims=True))
+    q *= size / np.sqrt((q * q).mean(axis=1, keepdims=True))
     want = 1.5 * rng.standard_normal((M, TOKENS)) * math.sqrt(128)
     return (q + want @ np.linalg.pinv(k).T).astype(np.float16)
 
