@@ -528,11 +528,14 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
     float qs[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) qs[cb] = ROPE ? unit : unit * kRawScale * qexp[cb];
-    float m[CB];  // running maxima of the raw products
+    // What a row's scores start from: the centre's share less the running maximum, so that the accumulators hold S - m. (Taken off
+    // afterwards it would have to be exact in the sum with the weights' shift: past 2^24 its rounding alone passes their range.)
+    float start[CB];
+    bool fresh = true;  // no maximum yet
     rc_f4 O[NV][CB], L[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-        m[cb] = -INFINITY;
+        start[cb] = base[cb];
         L[cb] = rc_f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < NV; ++n) O[n][cb] = L[cb];
@@ -722,7 +725,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
                 const v4i a = l0[t % kLo], b = l1[t % kLo];
                 const v8i lo = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_lo(lo, q8[cb], rc_f4{0.f, 0.f, 0.f, 0.f});
+                for (int cb = 0; cb < CB; ++cb) S[t][cb] = mfma_lo(lo, q8[cb], rc_f4{start[cb], start[cb], start[cb], start[cb]});
                 if (t + kLo < TB) low_part(t + kLo);
 #pragma unroll
                 for (int i = kAhead * t / TB; i < kAhead * (t + 1) / TB; ++i) kf[i] = key(i);
@@ -740,7 +743,7 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
 #pragma unroll
             for (int t = 0; t < TB; ++t)
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) S[t][cb] = rc_f4{base[cb], base[cb], base[cb], base[cb]};
+                for (int cb = 0; cb < CB; ++cb) S[t][cb] = rc_f4{start[cb], start[cb], start[cb], start[cb]};
             auto part = [&](auto first) {  // matrix steps `first` and `first` + 1
                 constexpr int s0 = decltype(first)::value;
                 rc_h8 kf[2 * TB], lw[2];
@@ -787,28 +790,26 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             for (int t = 0; t < TB; ++t)
 #pragma unroll
                 for (int v = 0; v < 4; ++v) top[cb] = fmaxf(top[cb], S[t][cb][v]);
-            raise = raise || (top[cb] - m[cb]) * qs[cb] > kTreeLazy;
+            raise = raise || top[cb] * qs[cb] > kTreeLazy;
         }
-        if (__any(raise)) {
+        if (__any(raise) || fresh) {
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
                 float t = fmaxf(top[cb], __shfl_xor(top[cb], 16));
                 t = fmaxf(t, __shfl_xor(t, 32));
-                if (t > m[cb]) {
-                    const float al = __builtin_amdgcn_exp2f((m[cb] - t) * qs[cb]);
-                    m[cb] = t;
-                    L[cb] *= al;
+                t = fresh ? (t == -INFINITY ? 0.f : t) : fmaxf(t, 0.f);  // (nothing seen: a part of a short last tile)
+                const float al = fresh ? 1.f : __builtin_amdgcn_exp2f(-t * qs[cb]);
+                start[cb] -= t;
+                L[cb] *= al;
 #pragma unroll
-                    for (int n = 0; n < NV; ++n) O[n][cb] *= al;
-                }
+                for (int n = 0; n < NV; ++n) O[n][cb] *= al;
+#pragma unroll
+                for (int i = 0; i < TB; ++i) S[i][cb] -= t;
             }
+            fresh = false;
         }
         // ---- weights and values: the second half's weights and operands while the first half multiplies
-        float off[CB];
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)  // a row that has seen no token yet (a part of a short last tile) has every weight 0
-            off[cb] = TW > 1 && m[cb] == -INFINITY ? 0.f : fmaf(-m[cb], qs[cb], kTreeShift);
-        auto weight = [&](int s, int cb, int e) { return __builtin_amdgcn_exp2f(fmaf(S[TB > 1 ? 2 * s + (e >> 2) : 0][cb][e & 3], qs[cb], off[cb])); };
+        auto weight = [&](int s, int cb, int e) { return __builtin_amdgcn_exp2f(fmaf(S[TB > 1 ? 2 * s + (e >> 2) : 0][cb][e & 3], qs[cb], kTreeShift)); };
         rc_h8 P[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
@@ -882,6 +883,9 @@ __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, c
             if (!late) __syncthreads();
         }
     }
+    float m[CB];  // maxima of the raw products; a row whose weights sum to nothing has seen no token
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) m[cb] = L[cb][0] == 0.f ? -INFINITY : base[cb] - start[cb];
     if constexpr (TW == 1) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {

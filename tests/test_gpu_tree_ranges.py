@@ -39,3 +39,31 @@ def test_rows_of_different_sizes(N, G):
     q[:, -1, -1] = 0
     got = run_tree(units, half(q), half(xk), half(xv), words, LENS, 200, 0.0)
     check(units, got, q, xk, xv, words, LENS, 0.0)
+
+
+@pytest.mark.parametrize("N,G", TREES)
+@pytest.mark.parametrize("base", [BASE, 0.0])
+@pytest.mark.parametrize("e", [6, 10, 14, 20])
+def test_logits_of_any_size_stay_finite(N, G, base, e):
+    # queries of the longest vectors that fp16 has, keys up to 2^20: logits to 2^36. One token takes all of a row.
+    units = ScaledUnits(ROWS, 300, 42, k_scale=2.0 ** e)
+    q, xk, xv, words = draw(units, N, G, 42)
+    q = (np.sign(q.astype(np.float32)) * 65504).astype(np.float16)
+    lens = [300, 130, 64]
+    got = run_tree(units, half(q), half(xk), half(xv), words, lens, 300, base).cpu().numpy().astype(np.float64)
+    assert np.isfinite(got).all()
+    clear = 0
+    for u in range(3):
+        k, v = units.keys(u, lens[u], base), units.values(u, lens[u])
+        qq = q[u].astype(np.float64).reshape(N * G, 128)
+        sees = np.array([[(int(words[u, n]) >> m) & 1 for m in range(N)] for n in range(N)], bool).repeat(G, axis=0)
+        s = np.concatenate([qq @ k.T, np.where(sees, qq @ xk[u].astype(np.float64).T, -np.inf)], axis=1) / np.sqrt(128)
+        # a logit is off by at most 2^-11 of the sum of its terms' sizes
+        err = 2.0 ** -11 * (np.abs(qq) @ np.abs(k).T).max(axis=1) / np.sqrt(128)
+        first = np.sort(s, axis=1)
+        sure = first[:, -1] - first[:, -2] > 2 * err + 30
+        want = np.concatenate([v, xv[u].astype(np.float64)])[s.argmax(axis=1)]
+        e_ = np.abs(got[u].reshape(N * G, 128) - want)[sure]
+        assert (e_ <= (2.0 ** -10 * np.abs(want) + 2.0 ** -18 * np.abs(want).max(axis=1, keepdims=True) + 2.0 ** -24)[sure]).all()
+        clear += int(sure.sum())
+    assert clear >= N * G  # a third of the rows at least
