@@ -394,7 +394,8 @@ int kvc_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stri
  *  out         device fp16 [n_units][n_tok][G][d], 16-byte aligned:
  *              out[u][n][g] = P_V^T sum_t p_t z_V,t + sum_m p_m xv_m,
  *              p = softmax over the visible t (q . k_t / sqrt(d)) and m (q . xk_m / sqrt(d));
- *              0 in a row that sees nothing.
+ *              0 in a row that sees nothing. Values past the fp16 range become +-65504 (a cached value near it is
+ *              reconstructed with up to half a step of error); NaN in a query makes its row NaN, and no other.
  *  ws          device workspace of >= kvc_tree_attn_workspace(...) bytes, 256-byte aligned, contents ignored.
  * Softmax statistics and sums are fp32; softmax weights are rounded to fp16, like the result, and rotated cached
  * keys to fp16 with a rest of two more bits. No atomics: results are deterministic. Async on `stream`.

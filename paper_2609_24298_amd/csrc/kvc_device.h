@@ -124,6 +124,15 @@ inline int device_cus() {
     return ncu;
 }
 
+// Four values rounded to fp16, to nearest even; past its largest number they become it, and what is no number stays none (a
+// median or an IEEE minNum would make one of it).
+typedef _Float16 sat_h4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ sat_h4 saturated_half(float x, float y, float z, float w) {
+    const _Float16 m = (_Float16)65504.f;
+    const sat_h4 h = {(_Float16)x, (_Float16)y, (_Float16)z, (_Float16)w}, most = {m, m, m, m};
+    return __builtin_elementwise_maximum(__builtin_elementwise_minimum(h, most), -most);
+}
+
 // Turns per position of the rotary pairs, base^(-2j/128) / 2 pi, j < 64: a product of two of sixteen powers each, so that a
 // call does not wait for 64 of them (two roundings of 2^-53).
 inline void rope_frequencies(float base, double* freq) {

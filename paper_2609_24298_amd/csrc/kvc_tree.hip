@@ -1238,9 +1238,8 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         if (col < R && row0 + col < wk.M) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-                const h4 h = {(_Float16)o[i][0], (_Float16)o[i][1], (_Float16)o[i][2], (_Float16)o[i][3]};
-                *reinterpret_cast<h4*>(out + ((int64_t)u * wk.M + row0 + col) * kD + 16 * (2 * wv + i) + 4 * grp) = h;
+                *reinterpret_cast<sat_h4*>(out + ((int64_t)u * wk.M + row0 + col) * kD + 16 * (2 * wv + i) + 4 * grp) =
+                    saturated_half(o[i][0], o[i][1], o[i][2], o[i][3]);
             }
         }
         row0 += R;

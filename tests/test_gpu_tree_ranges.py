@@ -7,7 +7,7 @@ torch = pytest.importorskip("torch")
 
 from test_gpu_tree import BASE, check, draw
 from tree_scales import ScaledUnits
-from verify_units import half, run_tree
+from verify_units import half, run_tree, tree_reference
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,34 @@ def test_logits_of_any_size_stay_finite(N, G, base, e):
         assert (e_ <= (2.0 ** -10 * np.abs(want) + 2.0 ** -18 * np.abs(want).max(axis=1, keepdims=True) + 2.0 ** -24)[sure]).all()
         clear += int(sure.sum())
     assert clear >= N * G  # a third of the rows at least
+
+
+@pytest.mark.parametrize("N,G", TREES)
+@pytest.mark.parametrize("base", [BASE, 0.0])
+def test_results_past_fp16_become_its_largest(N, G, base):
+    # values near the largest fp16 number, off by up to half a step of few bits after their reconstruction
+    units = ScaledUnits(ROWS, 200, 43, v_scale=2.0 ** 17)
+    q, xk, xv, words = draw(units, N, G, 43)
+    xv = np.clip(xv.astype(np.float32) * 2.0 ** 15, -65504, 65504).astype(np.float16)
+    words[:, -1] = 0
+    lens = np.array([1, 2, 0])
+    got = run_tree(units, half(q), half(xk), half(xv), words, lens, 200, base).cpu().numpy().astype(np.float64)
+    past = 0
+    for u in range(3):
+        ref, bound = tree_reference(units, u, q[u], xk[u], xv[u], words[u], int(lens[u]), base)
+        past += int((np.abs(ref) > 65504 + bound).sum())
+        assert (np.abs(got[u] - np.clip(ref, -65504, 65504)) <= bound).all(), u
+    assert past > 100
+
+
+def test_a_row_of_no_numbers_stays_one_and_alone():
+    units = ScaledUnits(ROWS, 200, 44)
+    for N, G in TREES:
+        for base in (BASE, 0.0):
+            q, xk, xv, words = draw(units, N, G, 44)
+            clean = run_tree(units, half(q), half(xk), half(xv), words, LENS, 200, base)
+            q[1, N // 2, 1] = np.nan
+            got = run_tree(units, half(q), half(xk), half(xv), words, LENS, 200, base)
+            assert got[1, N // 2, 1].isnan().all()
+            got[1, N // 2, 1] = clean[1, N // 2, 1]
+            assert torch.equal(got, clean), (N, G, base)
