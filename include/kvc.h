@@ -406,7 +406,8 @@ int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint
                   const uint64_t* mask, const int32_t* seq_len, int32_t max_seq_len, float rope_base, uint16_t* out,
                   void* ws, size_t ws_bytes, void* stream);
 
-/* Workspace bytes kvc_tree_attn needs (host only; 0 on an error). */
+/* Workspace bytes kvc_tree_attn needs (host only; 0 on an error). Never falls as G, n_tok, max_seq_len or the units grow: a
+ * workspace for the largest call serves every smaller one. */
 size_t kvc_tree_attn_workspace(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok,
                                int32_t max_seq_len);
 

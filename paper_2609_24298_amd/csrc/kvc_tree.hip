@@ -1251,8 +1251,10 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
 struct TreeLayout {
     TreeWork wk;
     int cb, rw;
-    int64_t acc, ml, total;
+    int64_t acc, ml;
 };
+
+int64_t round_up(int64_t x) { return (x + 255) / 256 * 256; }
 
 TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G, int n_tok, int max_seq, bool rope) {
     TreeLayout t;
@@ -1274,16 +1276,20 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.U = U;
     t.wk.n_blocks = (int)std::min<int64_t>(std::max(1, device_cus() * (tree_pair(t.cb, t.rw, rope) ? 2 : 1) / t.wk.nrb), (int64_t)U * (tiles ? tiles + start_cost(t.wk.M) : 0));
     const int64_t rows = t.wk.n_blocks ? ((int64_t)t.wk.n_blocks + U) * t.wk.M : 0;
-    auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
     t.acc = 0;
-    t.ml = up(rows * kD * 4);
-    t.total = std::max<int64_t>(t.ml + up(rows * 8), 256);
+    t.ml = round_up(rows * kD * 4);
     return t;
 }
 
-// What either form needs: more blocks, as plain keys may have, leave more pieces.
-int64_t tree_need(const kvc_stream_desc* k, const kvc_stream_desc* v, int G, int n_tok, int max_seq) {
-    return std::max(tree_layout(k, v, G, n_tok, max_seq, false).total, tree_layout(k, v, G, n_tok, max_seq, true).total);
+// What either form of the call needs, and every call of fewer rows, units or tokens, so that a server may take one workspace for
+// its largest: blocks times rows falls where a CU's second block or a whole row block no longer fits (past 64 rows, 256, 512, 768),
+// this bound of it does not. Rows of one block's pieces: 2 M for a CU up to 64 rows, then at least 128 and at most 256; a call of
+// few tiles has as many blocks as those, each unit's start counted as the most tiles that it may be.
+int64_t tree_need(const kvc_stream_desc* k, int G, int n_tok, int max_seq) {
+    const int64_t M = n_tok * G, U = k->n_units, tiles = ((int64_t)max_seq + kTile - 1) / kTile;
+    const int64_t a_cu = M <= 64 ? 2 * M : std::min<int64_t>(std::max<int64_t>(M, 128), 256);
+    const int64_t rows = tiles ? std::min(std::max(device_cus() * a_cu, M), U * (tiles + start_cost(0)) * M) + U * M : 0;
+    return std::max<int64_t>(round_up(rows * kD * 4) + round_up(rows * 8), 256);
 }
 
 template <int CB, int RW, bool ROPE>
@@ -1334,7 +1340,7 @@ using namespace kvc;
 extern "C" size_t kvc_tree_attn_workspace(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, int32_t n_tok, int32_t max_seq_len) {
     clear_error();
     if (tree_check(k, v, G, n_tok, max_seq_len)) return 0;
-    return (size_t)tree_need(k, v, G, n_tok, max_seq_len);
+    return (size_t)tree_need(k, G, n_tok, max_seq_len);
 }
 
 extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint16_t* q, int32_t G, int32_t n_tok,
@@ -1356,7 +1362,7 @@ extern "C" int kvc_tree_attn(const kvc_stream_desc* k, const kvc_stream_desc* v,
     if (!ws) return set_error(KVC_EINVAL, "kvc_tree_attn: null workspace");
     if (reinterpret_cast<uintptr_t>(ws) & 255) return set_error(KVC_EINVAL, "kvc_tree_attn: workspace not 256-byte aligned");
     const TreeLayout t = tree_layout(k, v, G, n_tok, max_seq_len, rope_base != 0.f);
-    if (const int64_t need = tree_need(k, v, G, n_tok, max_seq_len); (int64_t)ws_bytes < need)
+    if (const int64_t need = tree_need(k, G, n_tok, max_seq_len); (int64_t)ws_bytes < need)
         return set_error(KVC_ENOSPACE, "kvc_tree_attn: workspace %zu < %lld bytes", ws_bytes, (long long)need);
     float* acc = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + t.acc);
     float2* ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(ws) + t.ml);

@@ -225,7 +225,8 @@ class Cache:
         kvc.kvc_decode_step(self.K, self.V, xk, xv, t_new, q, self.w.group, seq_len, max_seq_len, out, ws, stream)
 
     def verify_buffers(self, n_tok: int, max_seq_len: int, sides=None):
-        """Workspace and output for verify() of n_tok drafted tokens per unit, of all units or of the units of `sides`."""
+        """Workspace and output for verify() of n_tok drafted tokens per unit, of all units or of the units of `sides`. The
+        workspace also serves fewer tokens, units or a smaller max_seq_len; the output is of n_tok tokens."""
         import torch
         K, V = sides or (self.K, self.V)
         nbytes = kvc.kvc_tree_attn_workspace(K, V, self.w.group, n_tok, max_seq_len)
