@@ -1401,7 +1401,7 @@ int decode_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, 
     if (max_seq_len > k->capacity || max_seq_len > v->capacity)
         return set_error(KVC_ENOSPACE, "kvc_decode_attn: max_seq_len exceeds capacity");
     // per-unit streams must lie inside their arenas (the kernels bound their loads by the stream)
-    const int64_t kct = ((int64_t)k->capacity + kTile - 1) / kTile, vct = ((int64_t)v->capacity + kTile - 1) / kTile;
+    const int64_t kct = tile_count(k->capacity), vct = tile_count(v->capacity);
     for (int u = 0; u < k->n_units; ++u) {
         if (kct * 8 * k->r_host[u] * k->b_host[u] > INT32_MAX || vct * 8 * v->r_host[u] * v->b_host[u] > INT32_MAX)
             return set_error(KVC_EUNSUPPORTED, "kvc_decode_attn: a unit's stream exceeds 2 GiB");
@@ -1495,7 +1495,7 @@ int decode_launch(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint
         hipLaunchKernelGGL(qprep_kernel<1>, dim3(U), dim3(64), qsm, st, K, q, G, LM, qa, qk);
     else
         hipLaunchKernelGGL(qprep_kernel<8>, dim3(U), dim3(512), qsm, st, K, q, G, LM, qa, qk);
-    const int kct = (k->capacity + kTile - 1) / kTile, vct = (v->capacity + kTile - 1) / kTile;
+    const int kct = tile_count(k->capacity), vct = tile_count(v->capacity);
     const dim3 grid(L.n_chunks, U, G / item_heads(G));
     int e = KVC_OK;
     switch (G) {

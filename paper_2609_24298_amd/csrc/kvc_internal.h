@@ -22,6 +22,9 @@ inline int64_t stream_bytes(int64_t n_tok, int r, int b) {
     return ((n_tok + KVC_TILE_TOKENS - 1) / KVC_TILE_TOKENS) * 8LL * r * b;
 }
 
+// Tiles of `tokens` tokens (in 64 bits: a narrow stream may hold up to 2^31 - 1).
+inline int tile_count(int32_t tokens) { return (int)(((int64_t)tokens + KVC_TILE_TOKENS - 1) / KVC_TILE_TOKENS); }
+
 // Elements of one lane of the bulk encoder that are coordinates of the unit, bit 4 nt + i for element i of
 // quarter nt, in a group of 16 coordinates of which the first `left` exist. Lane (col, grp) holds
 // coordinates 4 grp + i on the K side and coordinate col on the V side. Only these may be settled: the

@@ -245,7 +245,7 @@ extern "C" int kvc_reconstruct(const kvc_stream_desc* s, int32_t t0, int32_t n_t
     if (n_tok == 0 || s->n_units == 0) return KVC_OK;
     if (!out) return set_error(KVC_EINVAL, "kvc_reconstruct: null output");
     const int tile_first = t0 / kTile, n_tiles = (t0 + n_tok - 1) / kTile - tile_first + 1;
-    const int cap_tiles = (int)(((int64_t)s->capacity + kTile - 1) / kTile);
+    const int cap_tiles = tile_count(s->capacity);
     // Tiles per block: about two blocks for every place the chip has (two blocks of four wavefronts per
     // CU), a multiple of the four wavefronts; longer runs share one staging of the basis.
     const int64_t want = ((int64_t)s->n_units * n_tiles + 1023) / 1024;

@@ -436,7 +436,7 @@ int launch_rope_g(const kvc_stream_desc* k, const kvc_stream_desc* v, const uint
                   double log2_base, int stage_bytes, float* part, int* n_chunks, hipStream_t st) {
     using R = RopeShape<G>;
     const int U = k->n_units, tpu = (max_seq_len + kTile - 1) / kTile;
-    const int kct = (k->capacity + kTile - 1) / kTile, vct = (v->capacity + kTile - 1) / kTile;
+    const int kct = tile_count(k->capacity), vct = tile_count(v->capacity);
     const int wave_lds = R::kWave + (stage_bytes + 15) / 16 * 16;
     const size_t smem = (size_t)R::kShared + (size_t)R::kWaves * wave_lds;  // of the largest block
     if (smem > 64 * 1024) {

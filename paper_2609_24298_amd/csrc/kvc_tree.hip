@@ -1258,7 +1258,7 @@ int64_t round_up(int64_t x) { return (x + 255) / 256 * 256; }
 
 TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G, int n_tok, int max_seq, bool rope) {
     TreeLayout t;
-    const int U = k->n_units, tiles = (max_seq + kTile - 1) / kTile;
+    const int U = k->n_units, tiles = tile_count(max_seq);
     t.wk.M = n_tok * G;
     // Rows of a wavefront and wavefronts side by side in rows, the rest of the eight sharing a tile's tokens. Sixteen rows until
     // eight wavefronts have them, then 32, since making a tile's operands costs the same for any number of rows: 256 rows x 16k
@@ -1270,8 +1270,8 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.rows_pb = 16 * t.cb * t.rw;
     t.wk.nrb = (t.wk.M + t.wk.rows_pb - 1) / t.wk.rows_pb;
     t.wk.max_seq = max_seq;
-    t.wk.k_cap_tiles = (k->capacity + kTile - 1) / kTile;
-    t.wk.v_cap_tiles = (v->capacity + kTile - 1) / kTile;
+    t.wk.k_cap_tiles = tile_count(k->capacity);
+    t.wk.v_cap_tiles = tile_count(v->capacity);
     // One block for every CU (LDS or registers let no second one in), or two, as long as there are tiles for them.
     t.wk.U = U;
     t.wk.n_blocks = (int)std::min<int64_t>(std::max(1, device_cus() * (tree_pair(t.cb, t.rw, rope) ? 2 : 1) / t.wk.nrb), (int64_t)U * (tiles ? tiles + start_cost(t.wk.M) : 0));
@@ -1286,7 +1286,7 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
 // this bound of it does not. Rows of one block's pieces: 2 M for a CU up to 64 rows, then at least 128 and at most 256; a call of
 // few tiles has as many blocks as those, each unit's start counted as the most tiles that it may be.
 int64_t tree_need(const kvc_stream_desc* k, int G, int n_tok, int max_seq) {
-    const int64_t M = n_tok * G, U = k->n_units, tiles = ((int64_t)max_seq + kTile - 1) / kTile;
+    const int64_t M = n_tok * G, U = k->n_units, tiles = tile_count(max_seq);
     const int64_t a_cu = M <= 64 ? 2 * M : std::min<int64_t>(std::max<int64_t>(M, 128), 256);
     const int64_t rows = tiles ? std::min(std::max(device_cus() * a_cu, M), U * (tiles + start_cost(0)) * M) + U * M : 0;
     return std::max<int64_t>(round_up(rows * kD * 4) + round_up(rows * 8), 256);
@@ -1323,8 +1323,8 @@ int tree_check(const kvc_stream_desc* k, const kvc_stream_desc* v, int32_t G, in
     if (max_seq_len > k->capacity || max_seq_len > v->capacity)
         return set_error(KVC_ENOSPACE, "kvc_tree_attn: max_seq_len exceeds capacity");
     if (max_seq_len > INT32_MAX - kTile + 1) return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: max_seq_len past 2^31 - 64");
-    const int64_t kct = ((int64_t)k->capacity + kTile - 1) / kTile, vct = ((int64_t)v->capacity + kTile - 1) / kTile;
-    if ((int64_t)k->n_units * (((int64_t)max_seq_len + kTile - 1) / kTile + start_cost(0)) > INT32_MAX / 2)  // counted in 32 bits
+    const int64_t kct = tile_count(k->capacity), vct = tile_count(v->capacity);
+    if ((int64_t)k->n_units * (tile_count(max_seq_len) + start_cost(0)) > INT32_MAX / 2)  // counted in 32 bits
         return set_error(KVC_EUNSUPPORTED, "kvc_tree_attn: more than 2^30 tiles of 64 tokens");
     for (int u = 0; u < k->n_units; ++u)  // byte offsets inside a stream are 32 bits
         if (kct * 8 * k->r_host[u] * k->b_host[u] > INT32_MAX || vct * 8 * v->r_host[u] * v->b_host[u] > INT32_MAX)
