@@ -368,8 +368,8 @@ int kvc_reconstruct(const kvc_stream_desc* s, int32_t t0, int32_t n_tok, float* 
  *  k_out       device fp16 [n_seq kv_heads][n_tok][d]: the keys before rotation, what the encoder takes.
  *  k_rot       device fp16, same shape: the rotated keys, what kvc_tree_attn takes. Either may be NULL.
  *  v_out       device fp16, same shape: the values.
- * fp32 inside, one rounding to nearest even at the end; values past the fp16 range become +-65504 (the
- * encoder takes finite input). Outputs are 16-byte aligned and overlap no input. Async on `stream`.
+ * fp32 inside, one rounding to nearest even at the end; values past the fp16 range become +-65504, NaN stays
+ * NaN (the encoder takes finite input: a projection that holds one has to be dealt with by the caller). Outputs are 16-byte aligned and overlap no input. Async on `stream`.
  */
 int kvc_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                   int32_t dtype, int32_t n_seq, int32_t n_tok, int32_t kv_heads, int32_t G, const float* wq,

@@ -28,8 +28,6 @@ constexpr int kNrD = KVC_HEAD_DIM;
 constexpr int kNrThreads = 256;
 constexpr int64_t kNrCached = 128ll << 20;
 
-typedef _Float16 nr_h4 __attribute__((ext_vector_type(4)));
-
 struct NrArgs {
     const void* x[3];        // q, k, v: token-major rows of heads (null: absent)
     int64_t stride[3];       // elements between tokens
@@ -62,14 +60,12 @@ __device__ __forceinline__ float4 load4(const void* p, int64_t at) {
     }
 }
 
-// Rounded to nearest even; values past the largest fp16 number become it (the encoder takes finite input).
+// (The encoder takes finite input: what is too large is the largest number, NaN is left for the caller to see.)
 template <bool NT>
 __device__ __forceinline__ void store4(uint16_t* p, float4 v) {
-    const float m = 65504.f;
-    const nr_h4 h = {(_Float16)__builtin_amdgcn_fmed3f(v.x, -m, m), (_Float16)__builtin_amdgcn_fmed3f(v.y, -m, m),
-                     (_Float16)__builtin_amdgcn_fmed3f(v.z, -m, m), (_Float16)__builtin_amdgcn_fmed3f(v.w, -m, m)};
-    if constexpr (NT) __builtin_nontemporal_store(h, reinterpret_cast<nr_h4*>(p));
-    else *reinterpret_cast<nr_h4*>(p) = h;
+    const sat_h4 h = saturated_half(v.x, v.y, v.z, v.w);
+    if constexpr (NT) __builtin_nontemporal_store(h, reinterpret_cast<sat_h4*>(p));
+    else *reinterpret_cast<sat_h4*>(p) = h;
 }
 
 __device__ __forceinline__ float row_sum16(float v) {
@@ -127,7 +123,10 @@ __global__ __launch_bounds__(kNrThreads) void norm_rope_kernel(const NrArgs a) {
             store4<NT>(plain + row * kNrD + 4 * c, x);
             store4<NT>(plain + row * kNrD + 64 + 4 * c, y);
         }
-        if (turned) {
+        if (turned && !a.rotate) {  // (a pair's other element does not enter, not even times 0)
+            store4<NT>(turned + row * kNrD + 4 * c, x);
+            store4<NT>(turned + row * kNrD + 64 + 4 * c, y);
+        } else if (turned) {
             store4<NT>(turned + row * kNrD + 4 * c, float4{x.x * cs[0] - y.x * sn[0], x.y * cs[1] - y.y * sn[1], x.z * cs[2] - y.z * sn[2],
                                                            x.w * cs[3] - y.w * sn[3]});
             store4<NT>(turned + row * kNrD + 64 + 4 * c, float4{x.x * sn[0] + y.x * cs[0], x.y * sn[1] + y.y * cs[1],
