@@ -361,6 +361,7 @@ int kvc_reconstruct(const kvc_stream_desc* s, int32_t t0, int32_t n_tok, float* 
  *              projection. 16-byte aligned, strides multiples of 16 bytes. Each may be NULL, with its outputs.
  *  dtype       KVC_F16, KVC_BF16 or KVC_F32, of q, k and v alike.
  *  wq, wk      device f32 [d], 16-byte aligned: x is first normalised, y = x / sqrt(mean(x^2) + eps) * w; NULL: y = x.
+ *              Elements may be of any finite size. With eps = 0 a head of zeros is NaN.
  *  pos         device int32 [n_seq][n_tok]: positions (any value; tokens of a tree may share one).
  *  rope_base   as kvc_decode_attn_rope, or 0: no rotation (pos may then be NULL).
  *  q_out       device fp16 [n_seq kv_heads][n_tok][G][d]: the rotated queries (query head h G + g of unit
@@ -369,7 +370,8 @@ int kvc_reconstruct(const kvc_stream_desc* s, int32_t t0, int32_t n_tok, float* 
  *  k_rot       device fp16, same shape: the rotated keys, what kvc_tree_attn takes. Either may be NULL.
  *  v_out       device fp16, same shape: the values.
  * fp32 inside, one rounding to nearest even at the end; values past the fp16 range become +-65504, NaN stays
- * NaN (the encoder takes finite input: a projection that holds one has to be dealt with by the caller). Outputs are 16-byte aligned and overlap no input. Async on `stream`.
+ * NaN (the encoder takes finite input: a projection that holds one has to be dealt with by the caller).
+ * Outputs are 16-byte aligned and overlap no input. Async on `stream`.
  */
 int kvc_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                   int32_t dtype, int32_t n_seq, int32_t n_tok, int32_t kv_heads, int32_t G, const float* wq,

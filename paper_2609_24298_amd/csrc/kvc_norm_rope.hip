@@ -27,6 +27,7 @@ namespace {
 constexpr int kNrD = KVC_HEAD_DIM;
 constexpr int kNrThreads = 256;
 constexpr int64_t kNrCached = 128ll << 20;
+constexpr float kNrLeast = 0x1p-100f;  // squares that fp32 holds to fewer bits (below 2^-126) are nothing beside a mean of this
 
 struct NrArgs {
     const void* x[3];        // q, k, v: token-major rows of heads (null: absent)
@@ -76,6 +77,12 @@ __device__ __forceinline__ float row_sum16(float v) {
     return v;
 }
 
+__device__ __forceinline__ float row_max16(float v) {
+    for (int o = 1; o < 16; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+__device__ __forceinline__ float max4(float4 a) { return fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(a.z), fabsf(a.w))); }
+__device__ __forceinline__ float4 ldexp4(float4 a, int e) { return float4{ldexpf(a.x, e), ldexpf(a.y, e), ldexpf(a.z, e), ldexpf(a.w, e)}; }
 __device__ __forceinline__ float dot4(float4 a) { return fmaf(a.x, a.x, fmaf(a.y, a.y, fmaf(a.z, a.z, a.w * a.w))); }
 
 template <int DT, bool NT>
@@ -108,8 +115,17 @@ __global__ __launch_bounds__(kNrThreads) void norm_rope_kernel(const NrArgs a) {
         const int64_t at = tok * (kind == 0 ? a.stride[0] : (kind == 1 ? a.stride[1] : a.stride[2])) + (int64_t)h * kNrD + 4 * c;
         float4 x = load4<DT>(src, at), y = load4<DT>(src, at + 64);
         if (w) {
-            const float ms = row_sum16(dot4(x) + dot4(y)) * (1.f / kNrD);
-            const float s = 1.f / sqrtf(ms + a.eps);
+            float ms = fmaf(row_sum16(dot4(x) + dot4(y)), 1.f / kNrD, a.eps);
+            if (!(ms >= kNrLeast && ms < INFINITY)) {  // squares past fp32 or below its precision: again, the largest element in [1, 2)
+                const float big = row_max16(fmaxf(max4(x), max4(y)));
+                if (big > 0.f && big < INFINITY) {
+                    const int e = ilogbf(big);
+                    x = ldexp4(x, -e);
+                    y = ldexp4(y, -e);
+                    ms = fmaf(row_sum16(dot4(x) + dot4(y)), 1.f / kNrD, ldexpf(a.eps, -2 * e));
+                }
+            }
+            const float s = 1.f / sqrtf(ms);
             const float4 wx = *reinterpret_cast<const float4*>(w + 4 * c), wy = *reinterpret_cast<const float4*>(w + 64 + 4 * c);
             x = float4{x.x * s * wx.x, x.y * s * wx.y, x.z * s * wx.z, x.w * s * wx.w};
             y = float4{y.x * s * wy.x, y.y * s * wy.y, y.z * s * wy.z, y.w * s * wy.w};

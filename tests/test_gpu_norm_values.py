@@ -1,11 +1,13 @@
-"""kvc_norm_rope where a projection holds values that are no numbers."""
+"""kvc_norm_rope where a projection holds values that are no numbers, or whose squares leave the range of fp32. Bounds as in
+test_gpu_norm_rope."""
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
 from paper_2609_24298_amd import kvc
 
-from test_gpu_norm_rope import D, DT
+from test_gpu_norm_rope import D, DT, near, reference, unit_major
 
 pytestmark = pytest.mark.gpu
 S, N, KV, G = 2, 3, 2, 4
@@ -58,3 +60,28 @@ def test_what_is_no_number_stays_none(dtype, base, norm, bad):
             assert (t[h].isnan() | (t[h] == 0)).all() and t[h].isnan().any()
         else:
             assert (t[h].isnan() | (t[h].abs() == 65504)).all()
+
+
+@pytest.mark.parametrize("dtype,scale,eps", [("fp32", 1e20, 1e-6), ("fp32", 3e37, 1e-6), ("bf16", 1e30, 1e-6), ("bf16", 1e37, 0.0), ("fp32", 1e-25, 0.0),
+                                             ("fp32", 1e-37, 0.0), ("bf16", 1e-30, 1e-60), ("fp32", 1e-20, 1e-40), ("fp32", 1e-12, 0.0)])
+@pytest.mark.parametrize("base", [10000.0, 0.0])
+def test_squares_outside_fp32(dtype, scale, eps, base):
+    x, w, pos = inputs(dtype, 4, scale)
+    x[0, 0, :D] *= 1e-3  # heads of different sizes in a wavefront
+    x[1, 1, D:2 * D] = 0
+    x[1, 1, D] = x[0, 0, 0]  # a head of one element
+    o = call(x, w, eps, base, pos)
+    f = lambda a, b: x[:, :, a * D:b * D].double().cpu().numpy().reshape(S, N, b - a, D)  # noqa: E731
+    wn, p, eps32 = w.double().cpu().numpy(), pos.cpu().numpy(), float(np.float32(eps))
+    _, rq, mq = reference(f(0, KV * G), wn, eps32, p, base)
+    pk, rk, mk = reference(f(KV * G, KV * G + KV), wn, eps32, p, base)
+    near(o[0], unit_major(rq, KV), unit_major(mq, KV))
+    near(o[1], unit_major(pk, KV)[:, :, 0], unit_major(mk, KV)[:, :, 0])
+    near(o[2], unit_major(rk, KV)[:, :, 0], unit_major(mk, KV)[:, :, 0])
+
+
+def test_small_values_beside_eps_are_as_they_were():
+    # eps far above the squares: nothing to rescue, the result is x / sqrt(eps) w
+    x, w, pos = inputs("fp32", 5, 1e-30)
+    o = call(x, w, 1.0, 10000.0, pos)
+    assert all((t == 0).all() for t in o)
