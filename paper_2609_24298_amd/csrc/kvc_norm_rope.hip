@@ -10,9 +10,9 @@
 // rounding to fewer bits is the one to fp16 on the way out (the unrotated and the rotated key are both
 // rounded from the fp32 norm, not one from the other).
 //
-// Bound by memory where there is much of it: 16384 tokens of 48 heads 68 us, 436 MB at 6.4 TB/s (a large copy reaches 5.2 to
-// 5.4), with vector instructions 89 % of the time. One token 3.2 us, 488 tokens of 80 heads 8 us: latency, and less than a
-// call's 13 us on the host.
+// At two limits where there is much of it: 16384 tokens of 48 heads in bf16 68 us, 436 MB at 6.4 TB/s (a large copy reaches 5.2 to
+// 5.4), with vector instructions 95 % of the time; in fp32, 638 MB, 119 us at 5.4 TB/s and vector instructions 51 %. One token
+// 3.3 us, 488 tokens of 80 heads 8.3 us: latency, and less than a call's 13 us on the host.
 #include <hip/hip_runtime.h>
 
 #include <cmath>

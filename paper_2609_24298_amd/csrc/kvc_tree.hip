@@ -8,11 +8,15 @@
 //  tree_finish_kernel   per sixteen (or four) rows: merges the pieces, applies P_V, adds the drafted tokens.
 //
 // What bounds it (2 bits per dimension, 64 units of ragged lengths unless said, times of both kernels):
-//  256 rows x 32k  310 us, 690 TFLOP/s of score and value products: vector instructions 44 % of the time, matrix units 37 %, which
-//                  two wavefronts a SIMD (256 registers each) overlap only in part; the rest is waits of a step for the one before.
+//  256 rows x 32k  313 us, 560 TFLOP/s of score and value products (of 39 GFLOP more the rebuilt keys): vector instructions 44 % of
+//                  the time, matrix units 37 %, which two wavefronts a SIMD (256 registers each) overlap only in part; the rest is
+//                  waits of a step for the one before.
 //   64 rows x 128k, 8 units at 1/2 bit  108 us: the wavefronts that make the keys (rotation, splitting), the same for one row or
 //                  64; vector instructions 44 %, LDS 45 %, matrix units 23 %.
-//   52 rows x 16k, keys not rotated  75 us: the latency of a tile's steps; vector instructions 32 %, matrix units 19 %, LDS 23 %.
+//  128 rows x 16k  118 us: as these; vector instructions 44 %, LDS 44 %, matrix units 29 %. (128 registers: some sixty values that a
+//                  piece sets up are spilled.)
+//   52 rows x 16k, keys not rotated  69 us: the latency of a tile's steps; vector instructions 35 %, matrix units 20 %, LDS 25 %. 128
+//                  rows 101 us (30, 27, 22 %), 256 rows 154 us (34, 37, 15 %).
 //   20 rows x 300  17 us: two launches of 7 to 10 us, each a chain of four reads of memory.
 // (The bytes, at most 110 MB a call, are never the bound.)
 #define KVC_DECODE_PARTIALS_UNIT
@@ -279,13 +283,13 @@ static_assert(kTreeMid + kD * 4 <= kTreeBuf);
 constexpr int kBufLo = kTile * kD * 2, kTreeBufV = kBufLo + kTile * kD, kTreeBufBytes = kTreeBufV + kTile * kD * 2;
 constexpr int kTreeLead = kTreeBuf + 2 * kTreeBufBytes;  // the queries' leading bits, [wavefront][cb][2][lane], or two tiles' key codes
 // Plain keys and up to 64 rows: two blocks share a CU, each with half its registers and LDS. (The basis lies in the buffers, the
-// projected queries' low parts behind them: [row block][4][lane].) 32 rows x 32k x 64 units 122 -> 95 us, 64 rows x 128k x 8
-// units at 1/2 bit 83 -> 68, 52 rows x 16k x 64 units 79.7 and 79.9 (then 75 by sharing the projection).
+// projected queries' low parts behind them: [row block][4][lane].) Against one block, 32 rows x 16k x 64 units
+// 70 -> 56 us, x 32k 120 -> 89.5, 52 rows x 16k 79 -> 69; 8 units, 64 rows x 128k at 1/2 bit 80 -> 63.
 constexpr bool tree_pair(int cb, int rw, bool rope) { return !rope && cb == 1 && rw <= 4; }
 constexpr int kPairLow = 2 * kTile * kD * 4;
 // Rotated keys and up to 64 (128) rows: eight wavefronts make the tiles and four (eight) more attend, three (four) to a SIMD. Fewer
-// registers each, and what one waits for the others fill. Against eight that do both, 64 units: 32 rows x 4k 40.3 -> 36.6 us, 52
-// rows x 16k 112 -> 98, 100 rows x 16k 136 -> 122, x 4k 55.2 and 55.3; 8 units, 64 rows x 128k at 1/2 bit 127 -> 108. (32
+// registers each, and what one waits for the others fill. Against eight that do both, 64 units: 32 rows x 4k 43.6 -> 37.3 us, 52
+// rows x 16k 121 -> 95, 100 rows x 16k 130 -> 114, x 4k 53.4 -> 51.0; 8 units, 64 rows x 128k at 1/2 bit 132 -> 107. (32
 // rows a wavefront need more than 168 registers.)
 constexpr bool tree_split(int cb, int rw, bool rope) { return rope && cb == 1 && rw >= 4; }
 constexpr int tree_threads(int cb, int rw, bool rope) { return kTreeThreads + (tree_split(cb, rw, rope) ? 64 * rw : 0); }
@@ -304,12 +308,13 @@ constexpr int tree_smem(int cb, int rw, bool rope) {
 // a weight is the lane whose operand needs it.
 // A rotated key is fp16 and the rest of it bf8 at 2^11 times its size, met by the queries' leading bits (e5m2 is fp16's upper byte):
 // logits keep about 14 bits of the key for a quarter more matrix work, where fp16 alone would put an error of 2^-12 of
-// each coordinate into the weights.
+// each coordinate into the weights. (The query is cut, not rounded, to its upper byte: up to 2^-2 of a rest's share is lost, and
+// more below 2^-14, where an fp16 number has fewer leading bits. Measured, logits are a ninth as far off as with fp16 alone.)
 // Keys that are not rotated are not rebuilt: q . k = (P_K q) . z up to the step, so a piece begins by projecting its queries (kept
-// as the sum of two fp16, 2^-22 off; a query is taken at a scale of its own, its largest element in [1, 2), since the second
-// fp16 of a small one would be below that type's range: queries of 2^-13 lost up to 2^-8 of a logit otherwise), a wavefront makes tile t + 1 by unpacking half of a token block's codes, and the
-// products are of codes and projections. Twice the matrix steps for the scores, but the making is a quarter: 52 rows x 16k
-// x 64 units 115 us rebuilt, 78 so; 256 rows x 32k 335 and 274.
+// as the sum of two fp16, 2^-22 off; each query at a scale of its own, its largest element in [1, 2), since the second fp16 of
+// a small one would be below that type's range), a wavefront makes tile t + 1 by unpacking half of a token block's codes, and
+// the products are of codes and projections. Twice the matrix steps for the scores, but the making is a quarter: 52 rows x 16k
+// x 64 units 95 us rebuilt and rotated, 69 so; 256 rows x 16k 179 and 154.
 // NV: N-tiles of values, so that ranks up to 64 and 96 do no products for the rest.
 template <int CB, int RW, bool ROPE, int NV>
 __device__ __forceinline__ void tree_piece(const DevSide& K, const DevSide& V, const uint16_t* __restrict__ q, const TreeWork& wk,
@@ -1262,9 +1267,9 @@ TreeLayout tree_layout(const kvc_stream_desc* k, const kvc_stream_desc* v, int G
     t.wk.M = n_tok * G;
     // Rows of a wavefront and wavefronts side by side in rows, the rest of the eight sharing a tile's tokens. Sixteen rows until
     // eight wavefronts have them, then 32, since making a tile's operands costs the same for any number of rows: 256 rows x 16k
-    // x 64 units 178 us, in two blocks of 128 each making them 217; 128 rows 124 us, as 32 rows a wavefront, half of them idle,
-    // 138 (keys not rotated: 151 and 170, 96 and 108). As few wavefronts in rows as hold them: 52 rows 95 us in four (that only
-    // attend), 100 in eight; keys not rotated 75 and 78, and 32 rows 57 in two and 72 in four (rotated 94 and 92).
+    // x 64 units 179 us, in two blocks of 128 each making them 209; 128 rows 117 us, as 32 rows a wavefront, half of them idle,
+    // 139 (keys not rotated: 154 and 179, 101 and 111). As few wavefronts in rows as hold them: 52 rows 95 us in four (that only
+    // attend), 102 in eight; keys not rotated 69 and 81, and 32 rows 56 in two and 66 in four.
     t.cb = t.wk.M <= 128 ? 1 : 2;
     t.rw = t.wk.M > 64 ? 8 : (t.wk.M > 32 || rope ? 4 : 2);
     t.wk.rows_pb = 16 * t.cb * t.rw;
