@@ -1001,15 +1001,16 @@ constexpr int kFinX = kFinZ + kFinRows * kFinZPitch * 4;     // drafted values [
 constexpr int kFinXPitch = kD + 8;
 constexpr int kFinP = kFinX + KVC_TREE_MAX_TOKENS * kFinXPitch * 2;  // weights [16][72] fp16
 constexpr int kFinPPitch = KVC_TREE_MAX_TOKENS + 8;
-constexpr int kFinRed = kFinP + kFinRows * kFinPPitch * 2;   // maxima and sums of the wavefronts [2][4][16], row maxima [16], 1 / sums [16]
-constexpr int kFinCount = kFinRed + (2 * 4 * 16 + 32) * 4;    // [8] tiles
+constexpr int kFinRed = kFinP + kFinRows * kFinPPitch * 2;   // maxima and sums of the wavefronts [2][4][16], drafts' maxima, both parts' factors [16]
+constexpr int kFinCount = kFinRed + (2 * 4 * 16 + 48) * 4;    // [8] tiles
 constexpr int kFinSmem = kFinCount + 8 * 4;
 static_assert(kFinSmem <= 64 * 1024, "no attribute is set for it");
 
-// Block: R rows of one unit (columns of the products past R repeat the last row). z = sum_c acc_c 2^(m_c - M) over the unit's
-// pieces, the drafted tokens' weights 2^(s - M), out = (step_V P_V^T z + sum_m p_m xv_m) / l. With few rows in all, blocks
-// of four rows, whose threads also share the pieces. Bound by latency, a chain of four reads of memory (8 to 10 us up to 64
-// rows x 64 units), and at 256 rows by the pieces' 42 MB.
+// Block: R rows of one unit (columns of the products past R repeat the last row). Cached tokens: z = sum_c acc_c 2^(m_c - M) over
+// the unit's pieces, by its own sum l; drafted ones: weights p_m = 2^(s - D) of their own maximum D; out = a step_V P_V^T z / l +
+// b sum_m p_m xv_m, with the parts' factors a and b in fp32, so that neither part's fp16 operands lose bits where the other
+// takes nearly all of the weights. With few rows in all, blocks of four rows, whose threads also share the pieces. Bound by
+// latency, a chain of four reads of memory (8 to 10 us up to 64 rows x 64 units), and at 256 rows by the pieces' 42 MB.
 template <int R>
 __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, const uint16_t* __restrict__ q, int G, int n_tok,
                                                                   const uint16_t* __restrict__ xk, int64_t xk_stride,
@@ -1027,7 +1028,8 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
     _Float16* ps = reinterpret_cast<_Float16*>(sm + kFinP);
     float* red = reinterpret_cast<float*>(sm + kFinRed);
     float* big = red + 2 * 4 * 16;
-    float* inv = big + 16;
+    float* of_cache = big + 16;
+    float* of_drafts = of_cache + 16;
     uint32_t* count = reinterpret_cast<uint32_t*>(sm + kFinCount);  // tiles of all units and of those before u, by wavefront
     const int rv = uni(V.r[u]);
     const uint64_t live = n_tok == 64 ? ~0ull : (1ull << n_tok) - 1ull;
@@ -1172,16 +1174,8 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         top = fmaxf(top, __shfl_xor(top, 32));
         if (grp == 0) red[wv * 16 + col] = top;
         __syncthreads();
-        float M = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
-        M = fmaxf(M, Mp);
-        const float Mf = M == -INFINITY ? 0.f : M;
-        {
-            const float w = __builtin_amdgcn_exp2f(Mp - Mf);
-            l *= w;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] *= w;
-        }
-        if (mi == 0) big[mr] = Mf;
+        const float D = fmaxf(fmaxf(red[mr], red[16 + mr]), fmaxf(red[32 + mr], red[48 + mr]));
+        if (mi == 0) big[mr] = D == -INFINITY ? 0.f : D;
         __syncthreads();
         {
             const float Mc = big[min(col, R - 1)];
@@ -1198,16 +1192,21 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
         }
         __syncthreads();
         {
-            const float sum = l + ((red[64 + mr] + red[80 + mr]) + (red[96 + mr] + red[112 + mr]));
-            const float i = sum > 0.f ? 1.f / sum : 0.f;
-            if (mi == 0) inv[mr] = i;
+            const float M = fmaxf(D, Mp), ref = M == -INFINITY ? 0.f : M;
+            const float wc = __builtin_amdgcn_exp2f(Mp - ref), wd = __builtin_amdgcn_exp2f(D - ref);
+            const float sum = fmaf(wc, l, wd * ((red[64 + mr] + red[80 + mr]) + (red[96 + mr] + red[112 + mr])));
+            const float i = sum > 0.f ? 1.f / sum : 0.f, il = l > 0.f ? 1.f / l : 0.f;
+            if (mi == 0) {
+                of_cache[mr] = wc * l * i;
+                of_drafts[mr] = wd * i;
+            }
             if (cg == 0)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) zs[mr * kFinZPitch + 8 * mc + e] = z[e] * i;
+                for (int e = 0; e < 8; ++e) zs[mr * kFinZPitch + 8 * mc + e] = z[e] * il;
         }
         __syncthreads();
         const int zc = min(col, R - 1);
-        const float step = V.delta[u], rinv = inv[zc];
+        const float by_cache = V.delta[u] * of_cache[zc], by_drafts = of_drafts[zc];
         rc_f4 o[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -1238,7 +1237,7 @@ __global__ __launch_bounds__(kFinThreads) void tree_finish_kernel(DevSide V, con
                 t = mfma_h(a, b, t);
             }
 #pragma unroll
-            for (int v = 0; v < 4; ++v) o[i][v] = fmaf(c[v], step, t[v] * rinv);
+            for (int v = 0; v < 4; ++v) o[i][v] = fmaf(c[v], by_cache, t[v] * by_drafts);
         }
         if (col < R && row0 + col < wk.M) {
 #pragma unroll

@@ -98,3 +98,32 @@ def test_a_row_of_no_numbers_stays_one_and_alone():
             assert got[1, N // 2, 1].isnan().all()
             got[1, N // 2, 1] = clean[1, N // 2, 1]
             assert torch.equal(got, clean), (N, G, base)
+
+
+@pytest.mark.parametrize("base", [BASE, 0.0])
+@pytest.mark.parametrize("N,G", [(1, 1), (5, 4), (40, 4)])
+@pytest.mark.parametrize("gap", [6.0, 12.0, 18.0])
+@pytest.mark.parametrize("cached", [True, False])
+def test_a_small_share_keeps_its_bits(N, G, base, gap, cached):
+    # One side (cached or drafted) takes all but e^-gap of the weights and adds (next to) nothing to the result: what the other
+    # gives is right to its own size. Each row sees one draft, itself; all keys of its cache are nearly alike.
+    units = ScaledUnits(ROWS[:2], 130, 45, k_scale=2.0 ** -8, v_scale=2.0 ** 8 if cached else 2.0 ** -20)
+    rng = np.random.default_rng(45)
+    q = rng.standard_normal((2, N, G, 128)).astype(np.float16)
+    q[:, :, :] = q[:, :, :1]  # a token's heads alike, so that its draft's logit is one
+    q64 = q.astype(np.float64)
+    lens = np.array([130, 67])
+    xk = np.zeros((2, N, 128), np.float16)
+    for u in range(2):
+        top = (q64[u, :, 0] @ units.keys(u, lens[u], base).T).max(axis=1) + np.log(lens[u]) * np.sqrt(128)
+        want = top + (gap if cached else -gap) * np.sqrt(128)
+        xk[u] = (want / (q64[u, :, 0] ** 2).sum(axis=1))[:, None] * q64[u, :, 0]
+    xv = np.zeros((2, N, 128), np.float16) if cached else (rng.standard_normal((2, N, 128)) * 2.0 ** 10).astype(np.float16)
+    words = np.tile(np.uint64(1) << np.arange(N, dtype=np.uint64), (2, 1))
+    got = run_tree(units, half(q), half(xk), half(xv), words, lens, 130, base).cpu().numpy().astype(np.float64)
+    for u in range(2):
+        ref, _ = tree_reference(units, u, q[u], xk[u], xv[u], words[u], int(lens[u]), base)
+        size = np.abs(ref).max(axis=-1, keepdims=True)
+        # weights and result to half a step of fp16 each (2^-11, of the row's largest element for sums of many, and 2^-25 where the
+        # result is below 2^-14), a logit's own error by a key's rounding, 2^-12 |q * k| / sqrt(d) < 2^-12 here, and fp32's
+        assert (np.abs(got[u] - ref) <= (3 * 2.0 ** -11 + 2.0 ** -12) * size + 2.0 ** -25).all(), float((np.abs(got[u] - ref) / size).max())
